@@ -43,10 +43,14 @@ typedef enum {
     AQ_ERR_ALIGNMENT = 3,     /* a pointer is not 16-byte aligned */
     AQ_ERR_CUDA = 4,          /* a CUDA launch or runtime call failed */
     AQ_ERR_TIMEOUT = 5,       /* a bounded device-side wait gave up (reported via workspace) */
-    AQ_ERR_WORKSPACE = 6      /* workspace missing or smaller than the *_workspace_bytes query */
+    AQ_ERR_WORKSPACE = 6,     /* workspace missing or smaller than the *_workspace_bytes query */
+    AQ_ERR_CAPACITY = 7       /* a cache has too few free pages, or a sequence's table is full
+                                 (reported via workspace) */
 } aq_status;
 
-typedef enum { AQ_F16 = 0, AQ_BF16 = 1, AQ_F32 = 2 } aq_dtype;
+/* AQ_E4M3: 8-bit floats (1 sign, 4 exponent, 3 significand bits, largest value 448) with
+ * power-of-two scales; only for key-value caches and the output of aq_rmsnorm. */
+typedef enum { AQ_F16 = 0, AQ_BF16 = 1, AQ_F32 = 2, AQ_E4M3 = 3 } aq_dtype;
 
 /* Shape and storage types of one quantized layer (App. C lists the three stored parts:
  * codebooks, codes, per-output-unit scales). */
@@ -398,6 +402,153 @@ size_t aq_store_device_bytes(aq_store* store);
  * NULL: nothing (AQ_OK). Errors: AQ_ERR_CUDA if the synchronisation reported an error (the
  * store is released all the same). */
 aq_status aq_store_destroy(aq_store* store);
+
+/* ---------------------------------------------------------------- paged key-value cache
+ * (No counterpart in the paper: what a decoder needs between the products above to answer with a
+ * model stored as codebooks.) The keys and values of all layers of a model, in pages of
+ * page_tokens tokens that the sequences take from one pool. Token t of sequence s is slot
+ * t mod page_tokens of page tables[s][t / page_tokens], in every layer. All bookkeeping is on the
+ * device and changed by the calls below in stream order, so a decode loop needs no host
+ * synchronisation and can be captured in a CUDA graph.
+ *   - refs[p] is the number of sequences that hold page p; 0: the page is free. Allocation takes
+ *     the lowest free indices. lens[s] is the length of sequence s (0: the slot s is unused);
+ *     tables[s] holds its ceil(lens[s] / page_tokens) pages and -1 from there on.
+ *   - A page held by several sequences is full: a fork shares full pages and copies a partial
+ *     last page. Sequences only grow (until they are freed), so no shared page is ever written.
+ *   - 8-bit entries (dtype AQ_E4M3) have one scale per token and head, stored as the byte e + 127
+ *     of the power of two 2^e that the code is multiplied by; e is the smallest exponent with
+ *     max |x| <= 448 * 2^e, kept in [-60, 60], so that x / 2^e is exact and rounded once.
+ * Conditions found on the device (an index outside its range, a sequence listed twice, no free
+ * page) are recorded in the workspace's status word (aq_workspace_status). */
+typedef struct aq_kv_cache {
+    int32_t layers;         /* >= 1 */
+    int32_t num_pages;      /* pages of the pool, >= 1 */
+    int32_t page_tokens;    /* a power of two, 8..1024 */
+    int32_t kv_heads;       /* >= 1 */
+    int32_t head_dim;       /* a multiple of 16, 16..256 */
+    int32_t max_seqs;       /* sequence slots, >= 1 */
+    int32_t max_pages;      /* entries of a sequence's table, >= 1 (max_pages * page_tokens < 2^31) */
+    int32_t dtype;          /* AQ_F16, AQ_BF16 or AQ_E4M3 */
+    void* k;                /* device, [layers][num_pages][kv_heads][page_tokens][head_dim] of dtype */
+    void* v;                /* as k */
+    void* k_scales;         /* AQ_E4M3: device, uint8 [layers][num_pages][kv_heads][page_tokens]; */
+    void* v_scales;         /* otherwise NULL */
+    int32_t* tables;        /* device, [max_seqs][max_pages] */
+    int32_t* lens;          /* device, [max_seqs] */
+    int32_t* refs;          /* device, [num_pages] */
+} aq_kv_cache;
+
+/* Lists of sequences, counts, positions and pages below are device int32 arrays, 4-byte aligned;
+ * a NULL list of sequences means 0..n-1. n = 0 does nothing.
+ * Workspace of every aq_kv_* call but aq_kv_attend: aq_kv_workspace_bytes(cache) bytes of device
+ * memory, 16-byte aligned, zero-filled before first use (0 if the cache is invalid). Calls that
+ * change the cache are ordered by their stream and must not overlap other calls on the cache.
+ * Errors: AQ_ERR_INVALID_ARG (a NULL cache or pointer, sizes outside the ranges above, n < 0 or
+ * n > max_seqs where a sequence may be listed once), AQ_ERR_UNSUPPORTED (a head_dim or page_tokens
+ * that is not supported), AQ_ERR_ALIGNMENT, AQ_ERR_WORKSPACE, AQ_ERR_CUDA. */
+size_t aq_kv_workspace_bytes(const aq_kv_cache* cache);
+
+/* Empty the cache: every table entry -1, every length and reference count 0. */
+aq_status aq_kv_init(const aq_kv_cache* cache, void* stream);
+
+/* Lengthen sequence seqs[i] by counts[i] >= 0 tokens (NULL: one each), i < n, taking new pages
+ * where a token begins one: the lowest free pages, in the order of the list. The new slots are
+ * written by aq_kv_write. All or nothing: if an entry is invalid or listed twice
+ * (AQ_ERR_INVALID_ARG), a table is too short or too few pages are free (AQ_ERR_CAPACITY), the
+ * cache is left as it was and the status recorded. */
+aq_status aq_kv_reserve(const aq_kv_cache* cache, int n, const int32_t* seqs, const int32_t* counts,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Make the empty sequence dst[i] a copy of src[i], i < n: full pages are shared (one more
+ * reference), a partial last page is copied, in all layers, to a new one (the lowest free pages,
+ * in the order of the list). Sources are taken as they were before the call. All or nothing, as
+ * aq_kv_reserve; a dst that is not empty or listed twice is AQ_ERR_INVALID_ARG. */
+aq_status aq_kv_fork(const aq_kv_cache* cache, int n, const int32_t* src, const int32_t* dst,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Release sequences: their pages lose one reference each, their table entries become -1 and their
+ * length 0. An empty sequence, or one listed twice, is released once; an index outside the cache
+ * is skipped (AQ_ERR_INVALID_ARG recorded). */
+aq_status aq_kv_free(const aq_kv_cache* cache, int n, const int32_t* seqs, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Move the pool's pages together: with U pages in use, the k-th used page at an index >= U is
+ * copied, in all layers, to the k-th free page below U, and tables and reference counts follow.
+ * Pages from U on are free afterwards (their contents are left as they are).
+ *   used : device, receives U, or NULL. */
+aq_status aq_kv_compact(const aq_kv_cache* cache, int32_t* used, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* Copy page src[i] to page dst[i] in all layers, i < n (keys, values and scales; the bookkeeping
+ * is not touched). The dst pages are distinct and none of them is a src. Indices outside the pool
+ * are skipped (AQ_ERR_INVALID_ARG recorded). */
+aq_status aq_kv_copy_pages(const aq_kv_cache* cache, int n, const int32_t* src, const int32_t* dst,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Write n new keys and values into a layer: row i becomes token positions[i] of sequence seqs[i]
+ * (positions NULL: the sequence's last token), rounded once to the cache's type.
+ *   k, v       : device, n rows of [kv_heads][head_dim] of x_dtype (AQ_F16, AQ_BF16 or AQ_F32),
+ *                16-byte aligned
+ *   row_stride : elements from one row to the next, >= kv_heads * head_dim and a multiple of 8
+ *                (the keys and values may be parts of one wider matrix)
+ * No slot may be named twice. A row whose slot is not in the cache (a position outside
+ * 0..lens-1, an index out of range) is skipped and AQ_ERR_INVALID_ARG recorded. */
+aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t* seqs,
+                      const int32_t* positions, const void* k, const void* v, int x_dtype,
+                      int64_t row_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of one new token of each listed sequence over its cached tokens:
+ *     s_t = scale * q . k_t,  out = sum_t p_t v_t / sum_t p_t,  p_t = exp(s_t - max s),
+ *     lse = ln sum_t exp(s_t),       over t = max(0, L - window) .. L-1, L = lens[seqs[i]]
+ * Query head h reads kv head h / (q_heads / kv_heads). A sequence of length 0 gives zeros and
+ * lse = -inf. Cached tokens that are not seen (past the length, before the window) are not read.
+ *   q        : device, n rows of [q_heads][head_dim] of q_dtype, 16-byte aligned, q_stride
+ *              elements apart (>= q_heads * head_dim, a multiple of 8); q_dtype is the cache's
+ *              type, or AQ_F16 / AQ_BF16 for an AQ_E4M3 cache
+ *   q_heads  : a positive multiple of kv_heads
+ *   scale    : a finite number (usually head_dim^-0.5)
+ *   window   : tokens seen from the end, or 0 for all
+ *   out      : device, [n][q_heads][head_dim] of q_dtype
+ *   lse      : device, [n][q_heads] floats (4-byte aligned), or NULL
+ *   workspace: aq_kv_attend_workspace_bytes(cache, n, q_heads) bytes, 16-byte aligned,
+ *              zero-filled before first use; calls that may overlap must not share one.
+ * seqs may name a sequence several times; NULL needs n <= max_seqs. Two kernels per 512 entries:
+ * the cache is read once, in equal shares of 16- or 32-token chunks whatever the lengths are,
+ * then the shares' results are joined in the order of the tokens, so the result does not depend
+ * on scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
+ * the longest possible length, and AQ_ERR_INVALID_ARG recorded.
+ * Accuracy: scores, maxima, sums and accumulators are fp32; the softmax weights are rounded to
+ * the cache's 16-bit type (fp16 for AQ_E4M3) for the product with V: an error of at most 2^-8
+ * (bf16) or 2^-11 (fp16) of sum_t p_t |v_t| / sum_t p_t before out is rounded. */
+size_t aq_kv_attend_workspace_bytes(const aq_kv_cache* cache, int n, int q_heads);
+aq_status aq_kv_attend(const aq_kv_cache* cache, int layer, int n, const int32_t* seqs, const void* q,
+                       int q_dtype, int64_t q_stride, int q_heads, float scale, int window, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- RMS norm
+ * (No counterpart in the paper: the norm in front of a decoder's projections.)
+ *     h = x + residual,   y[r, c] = weight[c] * h[r, c] / sqrt(mean_c h[r, c]^2 + eps)
+ * computed in fp32; residual_out gets h and y gets y, each rounded once (y is taken from the h
+ * that was not rounded).
+ *   x            : device, rows of [cols] of x_dtype, x_stride elements apart (>= cols, a
+ *                  multiple of 8)
+ *   residual     : device, [rows][cols] of r_dtype, or NULL (h = x)
+ *   residual_out : device, [rows][cols] of r_dtype, or NULL; it may be residual, or x (with
+ *                  x_stride = cols and x_dtype = r_dtype)
+ *   weight       : device, [cols] of w_dtype
+ *   y            : device, [rows][cols] of y_dtype; AQ_F16, AQ_BF16, AQ_F32 or AQ_E4M3; it may
+ *                  be x (x_stride = cols, the same type) or residual (the same type) when they
+ *                  are not residual_out
+ *   y_scales     : AQ_E4M3: device, uint8 [rows][cols / scale_block] scale bytes as in the
+ *                  key-value cache; otherwise NULL
+ *   scale_block  : AQ_E4M3: 32 (cols then a multiple of 32), or cols (one scale per row)
+ * x, residual and weight types: AQ_F16, AQ_BF16 or AQ_F32. cols: a multiple of 8, 8..65536;
+ * eps >= 0. rows = 0 does nothing. Errors: AQ_ERR_INVALID_ARG, AQ_ERR_UNSUPPORTED (cols),
+ * AQ_ERR_ALIGNMENT, AQ_ERR_CUDA. */
+aq_status aq_rmsnorm(int rows, int cols, const void* x, int x_dtype, int64_t x_stride,
+                     const void* residual, void* residual_out, int r_dtype, const void* weight,
+                     int w_dtype, float eps, void* y, int y_dtype, void* y_scales, int scale_block,
+                     void* stream);
 
 /* ---------------------------------------------------------------- workspace helpers
  * aq_selftest_wait: self-test of the library's failure detection (no counterpart in the

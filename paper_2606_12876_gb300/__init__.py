@@ -14,8 +14,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libaq.so")
 
 AQ_OK, AQ_ERR_INVALID_ARG, AQ_ERR_UNSUPPORTED, AQ_ERR_ALIGNMENT = 0, 1, 2, 3
-AQ_ERR_CUDA, AQ_ERR_TIMEOUT, AQ_ERR_WORKSPACE = 4, 5, 6
-AQ_F16, AQ_BF16, AQ_F32 = 0, 1, 2
+AQ_ERR_CUDA, AQ_ERR_TIMEOUT, AQ_ERR_WORKSPACE, AQ_ERR_CAPACITY = 4, 5, 6, 7
+AQ_F16, AQ_BF16, AQ_F32, AQ_E4M3 = 0, 1, 2, 3
 AQ_LAYOUT_STATIC_WEIGHTS = 1
 DTYPES = {"f16": AQ_F16, "bf16": AQ_BF16, "f32": AQ_F32}
 TORCH_DTYPES = {AQ_F16: torch.float16, AQ_BF16: torch.bfloat16, AQ_F32: torch.float32}
@@ -29,7 +29,10 @@ EXPORTS = ["aq_abi_version", "aq_status_string", "aq_last_error", "aq_plane_byte
            "aq_store_planes", "aq_store_books", "aq_store_scales", "aq_store_device_bytes",
            "aq_store_destroy", "aq_wmse_workspace_bytes", "aq_wmse", "aq_beam_workspace_bytes",
            "aq_beam_search", "aq_selftest_wait", "aq_selftest_read", "aq_gemv_group_workspace_bytes",
-           "aq_gemv_group"]
+           "aq_gemv_group",
+           "aq_kv_workspace_bytes", "aq_kv_init", "aq_kv_reserve", "aq_kv_fork", "aq_kv_free",
+           "aq_kv_compact", "aq_kv_copy_pages", "aq_kv_write", "aq_kv_attend_workspace_bytes",
+           "aq_kv_attend", "aq_rmsnorm"]
 
 
 class AQError(RuntimeError):
@@ -51,6 +54,14 @@ class Layout(ctypes.Structure):
     @classmethod
     def make(cls, out, inp, M, B=8, G=8, book_dtype="f16", scale_dtype="f16", flags=0):
         return cls(out, inp, G, M, B, DTYPES[book_dtype], DTYPES[scale_dtype], flags)
+
+
+class KVCache(ctypes.Structure):
+    """struct aq_kv_cache (device pointers as integers)."""
+    _fields_ = [(f, ctypes.c_int32) for f in ("layers", "num_pages", "page_tokens", "kv_heads",
+                                              "head_dim", "max_seqs", "max_pages", "dtype")] + \
+               [(f, ctypes.c_void_p) for f in ("k", "v", "k_scales", "v_scales", "tables", "lens",
+                                               "refs")]
 
 
 _lib = None
@@ -104,6 +115,22 @@ def lib():
             "aq_wmse": (i32, [lp, vp, vp, vp, vp, vp, i32, ctypes.POINTER(ctypes.c_double), vp,
                               vp, sz, vp]),
         }
+        cp, i64, f32 = ctypes.POINTER(KVCache), ctypes.c_int64, ctypes.c_float
+        sig.update({
+            "aq_kv_workspace_bytes": (sz, [cp]),
+            "aq_kv_init": (i32, [cp, vp]),
+            "aq_kv_reserve": (i32, [cp, i32, vp, vp, vp, sz, vp]),
+            "aq_kv_fork": (i32, [cp, i32, vp, vp, vp, sz, vp]),
+            "aq_kv_free": (i32, [cp, i32, vp, vp, sz, vp]),
+            "aq_kv_compact": (i32, [cp, vp, vp, sz, vp]),
+            "aq_kv_copy_pages": (i32, [cp, i32, vp, vp, vp, sz, vp]),
+            "aq_kv_write": (i32, [cp, i32, i32, vp, vp, vp, vp, i32, i64, vp, sz, vp]),
+            "aq_kv_attend_workspace_bytes": (sz, [cp, i32, i32]),
+            "aq_kv_attend": (i32, [cp, i32, i32, vp, vp, i32, i64, i32, f32, i32, vp, vp, vp, sz,
+                                   vp]),
+            "aq_rmsnorm": (i32, [i32, i32, vp, i32, i64, vp, vp, i32, vp, i32, f32, vp, i32, vp,
+                                 i32, vp]),
+        })
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -316,6 +343,64 @@ def aq_gemv_group(layouts, m, planes, books, scales, x, x_dtype, batch, ys, y_dt
                                (vp * n)(*[_ptr(s) for s in scales]), _ptr(x), x_dtype, batch,
                                (vp * n)(*[_ptr(y) for y in ys]), y_dtype, _ptr(workspace),
                                workspace_bytes, _stream(stream)), "aq_gemv_group")
+
+
+def kv_workspace_bytes(cache):
+    return lib().aq_kv_workspace_bytes(ctypes.byref(cache))
+
+
+def kv_attend_workspace_bytes(cache, n, q_heads):
+    return lib().aq_kv_attend_workspace_bytes(ctypes.byref(cache), n, q_heads)
+
+
+def aq_kv_init(cache, stream=None):
+    _check(lib().aq_kv_init(ctypes.byref(cache), _stream(stream)), "aq_kv_init")
+
+
+def aq_kv_reserve(cache, n, seqs, counts, workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_reserve(ctypes.byref(cache), n, _ptr(seqs), _ptr(counts), _ptr(workspace),
+                               workspace_bytes, _stream(stream)), "aq_kv_reserve")
+
+
+def aq_kv_fork(cache, n, src, dst, workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_fork(ctypes.byref(cache), n, _ptr(src), _ptr(dst), _ptr(workspace),
+                            workspace_bytes, _stream(stream)), "aq_kv_fork")
+
+
+def aq_kv_free(cache, n, seqs, workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_free(ctypes.byref(cache), n, _ptr(seqs), _ptr(workspace), workspace_bytes,
+                            _stream(stream)), "aq_kv_free")
+
+
+def aq_kv_compact(cache, used, workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_compact(ctypes.byref(cache), _ptr(used), _ptr(workspace), workspace_bytes,
+                               _stream(stream)), "aq_kv_compact")
+
+
+def aq_kv_copy_pages(cache, n, src, dst, workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_copy_pages(ctypes.byref(cache), n, _ptr(src), _ptr(dst), _ptr(workspace),
+                                  workspace_bytes, _stream(stream)), "aq_kv_copy_pages")
+
+
+def aq_kv_write(cache, layer, n, seqs, positions, k, v, x_dtype, row_stride, workspace,
+                workspace_bytes, stream=None):
+    _check(lib().aq_kv_write(ctypes.byref(cache), layer, n, _ptr(seqs), _ptr(positions), _ptr(k),
+                             _ptr(v), x_dtype, row_stride, _ptr(workspace), workspace_bytes,
+                             _stream(stream)), "aq_kv_write")
+
+
+def aq_kv_attend(cache, layer, n, seqs, q, q_dtype, q_stride, q_heads, scale, window, out, lse,
+                 workspace, workspace_bytes, stream=None):
+    _check(lib().aq_kv_attend(ctypes.byref(cache), layer, n, _ptr(seqs), _ptr(q), q_dtype,
+                              q_stride, q_heads, scale, window, _ptr(out), _ptr(lse),
+                              _ptr(workspace), workspace_bytes, _stream(stream)), "aq_kv_attend")
+
+
+def aq_rmsnorm(rows, cols, x, x_dtype, x_stride, residual, residual_out, r_dtype, weight, w_dtype,
+               eps, y, y_dtype, y_scales, scale_block, stream=None):
+    _check(lib().aq_rmsnorm(rows, cols, _ptr(x), x_dtype, x_stride, _ptr(residual),
+                            _ptr(residual_out), r_dtype, _ptr(weight), w_dtype, eps, _ptr(y),
+                            y_dtype, _ptr(y_scales), scale_block, _stream(stream)), "aq_rmsnorm")
 
 
 def aq_selftest_read(src, nbytes, sink, stream=None):

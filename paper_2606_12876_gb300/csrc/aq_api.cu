@@ -132,6 +132,7 @@ const char* aq_status_string(int status) {
         case AQ_ERR_CUDA: return "CUDA error";
         case AQ_ERR_TIMEOUT: return "device-side wait timed out";
         case AQ_ERR_WORKSPACE: return "workspace missing or too small";
+        case AQ_ERR_CAPACITY: return "cache pages or table exhausted";
         default: return "unknown status";
     }
 }
