@@ -512,10 +512,10 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  *   lse      : device, [n][q_heads] floats (4-byte aligned), or NULL
  *   workspace: aq_kv_attend_workspace_bytes(cache, n, q_heads) bytes, 16-byte aligned,
  *              zero-filled before first use; calls that may overlap must not share one.
- * seqs may name a sequence several times; NULL needs n <= max_seqs. Two kernels per 512 entries:
- * the cache is read once, in equal shares of 16- or 32-token chunks whatever the lengths are,
- * then the shares' results are joined in the order of the tokens, so the result does not depend
- * on scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
+ * seqs may name a sequence several times; NULL needs n <= max_seqs. One kernel per 512 entries:
+ * the cache is read once, in equal shares of 16- or 32-token chunks whatever the lengths are, and
+ * the shares' results are joined in the order of the tokens, so the result does not depend on
+ * scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
  * the longest possible length, and AQ_ERR_INVALID_ARG recorded.
  * Accuracy: scores, maxima, sums and accumulators are fp32; the softmax weights are rounded to
  * the cache's 16-bit type (fp16 for AQ_E4M3) for the product with V: an error of at most 2^-8

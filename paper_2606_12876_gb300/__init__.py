@@ -155,6 +155,19 @@ def _ptr(t):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _stream_of(index):
+    """The raw current stream of CUDA device `index`, which must be the current device (a launch
+    on another device's stream would not reach its tensors)."""
+    if (torch.cuda.current_device() if _raw_device is None else _raw_device()) != index:
+        raise ValueError("the tensors are on cuda:%d, which is not the current device" % index)
+    if _raw_stream is not None:
+        return _raw_stream(index)
+    return torch.cuda.current_stream().cuda_stream
+
+
 def _stream(stream):
     if stream is None:
         if _raw_stream is not None:
@@ -382,25 +395,22 @@ def aq_kv_copy_pages(cache, n, src, dst, workspace, workspace_bytes, stream=None
                                   workspace_bytes, _stream(stream)), "aq_kv_copy_pages")
 
 
-def aq_kv_write(cache, layer, n, seqs, positions, k, v, x_dtype, row_stride, workspace,
-                workspace_bytes, stream=None):
-    _check(lib().aq_kv_write(ctypes.byref(cache), layer, n, _ptr(seqs), _ptr(positions), _ptr(k),
-                             _ptr(v), x_dtype, row_stride, _ptr(workspace), workspace_bytes,
-                             _stream(stream)), "aq_kv_write")
+# The three calls of a decode step's inner loop take addresses and the raw stream as integers and
+# return the status: their callers (kv.py, norm.py) have them at hand, and on small batches the
+# host's time per call is what counts.
+def aq_kv_write(*args):
+    """aq_kv_write of aq.h; a cache is passed as ctypes.byref(KVCache). Returns the status."""
+    return (_lib or lib()).aq_kv_write(*args)
 
 
-def aq_kv_attend(cache, layer, n, seqs, q, q_dtype, q_stride, q_heads, scale, window, out, lse,
-                 workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_attend(ctypes.byref(cache), layer, n, _ptr(seqs), _ptr(q), q_dtype,
-                              q_stride, q_heads, scale, window, _ptr(out), _ptr(lse),
-                              _ptr(workspace), workspace_bytes, _stream(stream)), "aq_kv_attend")
+def aq_kv_attend(*args):
+    """aq_kv_attend of aq.h; a cache is passed as ctypes.byref(KVCache). Returns the status."""
+    return (_lib or lib()).aq_kv_attend(*args)
 
 
-def aq_rmsnorm(rows, cols, x, x_dtype, x_stride, residual, residual_out, r_dtype, weight, w_dtype,
-               eps, y, y_dtype, y_scales, scale_block, stream=None):
-    _check(lib().aq_rmsnorm(rows, cols, _ptr(x), x_dtype, x_stride, _ptr(residual),
-                            _ptr(residual_out), r_dtype, _ptr(weight), w_dtype, eps, _ptr(y),
-                            y_dtype, _ptr(y_scales), scale_block, _stream(stream)), "aq_rmsnorm")
+def aq_rmsnorm(*args):
+    """aq_rmsnorm of aq.h. Returns the status."""
+    return (_lib or lib()).aq_rmsnorm(*args)
 
 
 def aq_selftest_read(src, nbytes, sink, stream=None):

@@ -122,7 +122,7 @@ aq_status launch_kv_copy_pages(const aq_kv_cache& c, int n, const int* src, cons
                                cudaStream_t st);
 aq_status launch_kv_write(const aq_kv_cache& c, int layer, int n, const int* seqs, const int* positions,
                           const void* k, const void* v, int x_dt, long long stride, void* ws, cudaStream_t st);
-size_t kv_attend_ws_bytes(const aq_kv_cache& c);
+size_t kv_attend_ws_bytes(const aq_kv_cache& c, int q_heads);
 aq_status launch_kv_attend(const aq_kv_cache& c, const DeviceInfo& di, int layer, int n, const int* seqs,
                            const void* q, int q_dt, long long q_stride, int q_heads, float scale, int window,
                            void* out, float* lse, void* ws, cudaStream_t st);

@@ -138,14 +138,14 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
 
 size_t aq_kv_attend_workspace_bytes(const aq_kv_cache* cache, int n, int q_heads) {
     if (check_cache(cache) != AQ_OK || n < 0 || q_heads < 1 || q_heads % cache->kv_heads) return 0;
-    return aq::kv_attend_ws_bytes(*cache);
+    return aq::kv_attend_ws_bytes(*cache, q_heads);
 }
 
 aq_status aq_kv_attend(const aq_kv_cache* cache, int layer, int n, const int32_t* seqs, const void* q, int q_dtype,
                        int64_t q_stride, int q_heads, float scale, int window, void* out, float* lse, void* workspace,
                        size_t workspace_bytes, void* stream) {
     if (aq_status st = check_call(cache, n, INT_MAX, {seqs, lse}, workspace, workspace_bytes,
-                                  cache && check_cache(cache) == AQ_OK ? aq::kv_attend_ws_bytes(*cache) : 0);
+                                  aq_kv_attend_workspace_bytes(cache, 0, q_heads));
         st != AQ_OK)
         return st;
     if (aq_status st = check_pools(cache); st != AQ_OK) return st;

@@ -7,18 +7,20 @@
 // Bound: every cached key and value is read once, 4 * head_dim bytes per token and head with
 // 16-bit entries, for 4 * head_dim * (query heads per kv head) operations: a few operations per
 // byte, so HBM is the limit and the work is arranged around keeping loads in flight.
-//   - A tile is up to 16 query heads that share a kv head; mma.sync m16n8k16 takes the heads as
-//     its rows. (At the copy bandwidth an SM receives 24 bytes a cycle, which asks for about 190
-//     multiply-adds a cycle of the padded 16-row tile; the legacy tensor path has several times
-//     that, and its fragments come straight from the copied tiles, so tensor memory would add
-//     waits and nothing else.)
+//   - A tile is the up to 8 (or 16) query heads that share a kv head. mma.sync m16n8k16 takes 16
+//     cached tokens as rows and 8 heads as columns, S^T = K Q^T, then 16 head dimensions as rows,
+//     O^T += V^T P^T: both big operands come straight from the copied tiles (ldmatrix), the
+//     weights change from one form to the other by an 8x8 transpose in registers, and a column's
+//     statistics are per-lane values. (At the copy bandwidth an SM receives 24 bytes a cycle,
+//     which asks for about 100 multiply-adds a cycle of an 8-head tile; the legacy tensor path has
+//     several times that, so tensor memory would add waits and nothing else.)
 //   - The work is the list of all (sequence, tile) segments cut into chunks of CT tokens; every
-//     warp takes an equal, contiguous share of the list whatever the sequences' lengths, and runs
-//     through it with a ring of asynchronous copies of its own that crosses segment ends: no
-//     CTA-wide step until the end.
+//     warp takes an equal, contiguous share of the list whatever the sequences' lengths (a segment
+//     counts SEG chunks more, for its query and its end), and runs through it with a ring of
+//     asynchronous copies of its own that crosses segment ends: no CTA-wide step until the end.
 //   - A segment that lies in one warp's share is written at once. Pieces of segments are merged
-//     per CTA, and what crosses CTAs is joined by a second kernel, in the order of the tokens, so
-//     the result does not depend on scheduling.
+//     per CTA; of the CTAs that a segment crosses, the last to finish joins their partials, in the
+//     order of the tokens, so the result does not depend on scheduling.
 //
 // Numbers: products of 16-bit values are accumulated in fp32 by the tensor cores; the statistics
 // and accumulators are fp32. The weights p_t are rounded to the cache's 16-bit type for the
@@ -28,19 +30,22 @@
 // multiplies its score; a value's scale 2^b multiplies its weight, with the running maximum taken
 // over s_t log2 e + b so that the fp16 weights stay in [0, 1].
 #include <atomic>
+#include <climits>
 
 #include "kv.cuh"
 
 namespace aq {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
+// One CTA per SM. The workspace is sized for the largest grid, so that its query needs no device.
+constexpr int kMaxCtas = 160;
+constexpr size_t kArrivedBytes = 2048;                       // three counters per CTA
+static_assert(kArrivedBytes >= 3 * kMaxCtas * 4, "room for the counters");
 constexpr int kSliceSeqs = 512;       // sequences per launch (their offsets sit in shared memory)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Sizes for a cache type and a padded head dimension HD (64, 128 or 256).
-template <int DT, int HD>
+// Sizes for a cache type, a padded head dimension HD (64, 128 or 256) and NH groups of 8 heads.
+template <int DT, int HD, int NH>
 struct Tile {
     static constexpr int ESZ = DT == AQ_E4M3 ? 1 : 2;
     static constexpr int RB = HD * ESZ;                      // bytes of a token's row
@@ -50,11 +55,15 @@ struct Tile {
     static constexpr int STAGE = 2 * KV + (ESZ == 1 ? 128 : 0);   // keys, values, scale bytes
     static constexpr int NS = STAGE <= 4224 ? 6 : HD == 256 && ESZ == 1 ? 5 : 3;
     static constexpr int RING = NS * STAGE;                  // a warp's ring
-    static constexpr int PART = 32 + 16 * HD;                // floats of a partial: max, sum, o
+    static constexpr int ROWS = 8 * NH;                      // query heads of a tile
+    static constexpr int OS = HD + 4;                        // floats from one row of a partial's o to the next
+    static constexpr int PART = 2 * ROWS + ROWS * OS;        // floats of a partial: maxima, sums, o
     static_assert(RING >= PART * 4, "a warp's ring holds its last partial");
-    static constexpr int CTAS = HD == 256 ? 1 : 2;           // per SM
-    static constexpr int SMEM = kWarps * RING;
+    static constexpr int WARPS = HD == 256 ? 4 : 8;
+    static constexpr int THREADS = 32 * WARPS;
+    static constexpr int SMEM = WARPS * RING;
 };
+constexpr int SEG = 2;                                       // chunks that a segment's start and end count for
 
 struct Args {
     const uint8_t *k, *v, *ks, *vs;   // the layer's pools
@@ -63,9 +72,9 @@ struct Args {
     void* out;
     float* lse;
     unsigned int* status;
-    float* part;                      // [CTA][2][PART], then [CTA * warps][PART] for first pieces
-    float* first;
-    long long* base;                  // [n + 1] offsets, for the join
+    int* arrived;                     // CTAs that have left their partial, by segment or group; 0 between calls
+    float* part;                      // [CTA][2][PART]: partials of segments that cross CTAs
+    float* first;                     // [CTA * warps][PART]: first pieces of the warps' shares
     long long q_stride;
     float scale;
     int n, q_heads, kv_heads, group, tiles_per_head, head_dim, page_log2, num_pages, max_seqs, max_pages, window, q_dt;
@@ -94,6 +103,12 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 __device__ __forceinline__ uint32_t widen_e4m3x2(uint32_t w) {
     uint32_t d;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((unsigned short)w));
+    return d;
+}
+// The transpose of an 8x8 matrix of 16-bit values (a lane holds a pair of row lane / 4).
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
 // 16 bytes global -> shared; zeros when take is false (nothing is read then).
@@ -141,17 +156,24 @@ __device__ __forceinline__ int chunks_of(int len, int lo) {
     return len > 0 ? (len - 1) / CT - lo / CT + 1 : 0;
 }
 
-// A place in the list of chunks.
+// a / b for non-negative a and positive b, in 32 bits where they fit.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
+// A place in the list of chunks. Positions count SEG for the start of every segment, then its
+// chunks; base[i] is the position of entry i's first segment.
 struct Place {
-    int i, tile, seq, len, lo;        // sequence entry, tile and its range
+    int i, tile, seq, len, lo;        // entry, tile, and the entry's sequence and range
     int t;                            // first token of the chunk
     int left;                         // chunks of the segment from here on
+    long long pos;
 };
 
-// The segment that holds chunk u, and the place of u in it (base: chunk offsets of the n entries).
+// The first chunk at or after position u (< the list's end; entry ranges as scanned).
 template <int CT>
-__device__ void place_at(const Args& a, const long long* base, const int2* range, const int* seq_of, int tiles,
-                         long long u, Place& p) {
+__device__ void place_at(const Args& a, const long long* base, const int2* range, const int* seq_of, long long u,
+                         Place& p) {
     int lo = 0, hi = a.n - 1;
     while (lo < hi) {                 // the last entry that starts at or before u
         const int mid = (lo + hi + 1) >> 1;
@@ -159,16 +181,21 @@ __device__ void place_at(const Args& a, const long long* base, const int2* range
         else hi = mid - 1;
     }
     const int2 r = range[lo];
-    const int per = chunks_of<CT>(r.x, r.y);
+    const int chunks = chunks_of<CT>(r.x, r.y), per = chunks + SEG;
     const long long in = u - base[lo];
-    const int tile = (int)(in / per), c = (int)(in - (long long)tile * per);
+    const int tile = (int)quotient(in, per);
+    const int c = max((int)(in - (long long)tile * per) - SEG, 0);
     p.i = lo, p.tile = tile, p.seq = seq_of[lo], p.len = r.x, p.lo = r.y;
     p.t = (r.y / CT + c) * CT;
-    p.left = per - c;
+    p.left = chunks - c;
+    p.pos = base[lo] + (long long)tile * per + SEG + c;
 }
-// To the next chunk of the list (there is one).
+__device__ __forceinline__ long long next_pos(const Place& p) { return p.pos + (p.left > 1 ? 1 : 1 + SEG); }
+
+// To the next chunk of the list (there is one). True: it begins a segment.
 template <int CT>
 __device__ __forceinline__ bool advance(const Args& a, const int2* range, const int* seq_of, int tiles, Place& p) {
+    p.pos = next_pos(p);
     if (--p.left > 0) {
         p.t += CT;
         return false;
@@ -185,37 +212,41 @@ __device__ __forceinline__ bool advance(const Args& a, const int2* range, const 
     return true;
 }
 
-// Scores, weights and output of one segment as far as a warp has read it. Rows: lane / 4 and that
-// + 8; the running maximum (of s_t log2 e + b) is the same in a row's four lanes, the sums are
-// each lane's own columns'.
-template <int HD>
+// One segment as far as a warp has read it. A lane's columns are the heads 8 g + 2 (lane % 4) + x;
+// m is the running maximum (of s_t log2 e + b), the same in a column's eight lanes; l the sum over
+// the lane's own tokens. o[g][j][y] belongs to head column y & 1 and dimension dim_of(j, y >> 1).
+template <int HD, int NH>
 struct Acc {
-    float o[HD / 8][4];
-    float m[2], l[2];
+    float o[NH][HD / 16][4];
+    float m[NH][2], l[NH][2];
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int j = 0; j < HD / 8; ++j)
+        for (int g = 0; g < NH; ++g) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[j][x] = 0.0f;
-        m[0] = m[1] = -INFINITY;
-        l[0] = l[1] = 0.0f;
+            for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) o[g][j][y] = 0.0f;
+            m[g][0] = m[g][1] = -INFINITY;
+            l[g][0] = l[g][1] = 0.0f;
+        }
     }
 };
-
-// The head dimension that o[j][x] of a lane with lane % 4 == q belongs to (x = 0, 1; 2 and 3 are
-// the same columns of the other row). E4M3 tiles pair the even and the odd columns of 16.
+// E4M3 tiles take the even dimensions of 16 as rows 0..7 and the odd ones as rows 8..15.
 template <int DT>
-__device__ __forceinline__ int column_of(int j, int x, int q) {
-    return DT == AQ_E4M3 ? 16 * (j >> 1) + 4 * q + 2 * x + (j & 1) : 8 * j + 2 * q + x;
+__device__ __forceinline__ int dim_of(int j, int half, int lane) {
+    return DT == AQ_E4M3 ? 16 * j + 2 * (lane >> 2) + half : 16 * j + 8 * half + (lane >> 2);
 }
 
-__device__ __forceinline__ float quad_sum(float v) {
-    v += __shfl_xor_sync(~0u, v, 1);
-    return v + __shfl_xor_sync(~0u, v, 2);
+// Over the eight lanes that share a column.
+__device__ __forceinline__ float column_sum(float v) {
+    v += __shfl_xor_sync(~0u, v, 4);
+    v += __shfl_xor_sync(~0u, v, 8);
+    return v + __shfl_xor_sync(~0u, v, 16);
 }
-__device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __shfl_xor_sync(~0u, v, 1));
-    return fmaxf(v, __shfl_xor_sync(~0u, v, 2));
+__device__ __forceinline__ float column_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(~0u, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(~0u, v, 8));
+    return fmaxf(v, __shfl_xor_sync(~0u, v, 16));
 }
 
 // Two adjacent output elements of a query row.
@@ -223,120 +254,208 @@ __device__ __forceinline__ void store_out2(const Args& a, size_t q_row, int col,
     uint32_t* o = (uint32_t*)((uint16_t*)a.out + q_row * a.head_dim + col);
     *o = a.q_dt == AQ_F16 ? round_pack2<AQ_F16>(v0, v1) : round_pack2<AQ_BF16>(v0, v1);
 }
+// 1 / sum; nothing seen (0) gives zeros, NaN stays NaN.
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.0f ? 1.0f / l : l; }
 __device__ __forceinline__ float lse_of(float m, float l) {
-    return l > 0.0f ? kLn2 * (m + log2f(l)) : -INFINITY;
+    return l > 0.0f ? kLn2 * (m + log2f(l)) : l == 0.0f ? -INFINITY : l;
 }
 
-// The query rows of (entry i, tile): first query head and how many of the 16 rows are real.
+// The query rows of a tile: first query head and how many there are.
+template <int ROWS>
 __device__ __forceinline__ void tile_rows(const Args& a, int tile, int* head0, int* rows) {
     const int kvh = tile / a.tiles_per_head, sub = tile - kvh * a.tiles_per_head;
-    *head0 = kvh * a.group + sub * 16;
-    *rows = min(16, a.group - sub * 16);
+    *head0 = kvh * a.group + sub * ROWS;
+    *rows = min(ROWS, a.group - sub * ROWS);
 }
 
-template <int DT, int HD>
-__device__ __forceinline__ void write_final(const Args& a, const Place& p, Acc<HD>& acc, int lane) {
+// A finished segment to the output: the 16-bit values are transposed back to rows of heads.
+template <int DT, int HD, int NH>
+__device__ __forceinline__ void write_final(const Args& a, const Place& p, Acc<HD, NH>& acc, int lane) {
     int head0, rows;
-    tile_rows(a, p.tile, &head0, &rows);
-    const int g = lane >> 2, q = lane & 3;
+    tile_rows<8 * NH>(a, p.tile, &head0, &rows);
+    const int q = lane & 3;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const float l = quad_sum(acc.l[h]);
-        const int r = g + 8 * h;
-        if (r >= rows) continue;
-        const size_t q_row = (size_t)p.i * a.q_heads + head0 + r;
-        const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;   // NaN stays NaN
-        if (a.lse && q == 0) a.lse[q_row] = l == l ? lse_of(acc.m[h], l) : l;
+    for (int g = 0; g < NH; ++g) {
+        float inv[2];
 #pragma unroll
-        for (int j = 0; j < HD / 8; j += DT == AQ_E4M3 ? 2 : 1) {
-            if constexpr (DT == AQ_E4M3) {
-                const int col = column_of<DT>(j, 0, q);
-                if (col < a.head_dim) {
-                    store_out2(a, q_row, col, acc.o[j][2 * h] * inv, acc.o[j + 1][2 * h] * inv);
-                    store_out2(a, q_row, col + 2, acc.o[j][2 * h + 1] * inv, acc.o[j + 1][2 * h + 1] * inv);
+        for (int x = 0; x < 2; ++x) {
+            const float l = column_sum(acc.l[g][x]);
+            const int r = 8 * g + 2 * q + x;
+            if (a.lse && lane < 4 && r < rows) a.lse[(size_t)p.i * a.q_heads + head0 + r] = lse_of(acc.m[g][x], l);
+            inv[x] = inverse_sum(l);
+        }
+        const int r = 8 * g + (lane >> 2);
+        uint16_t* out = (uint16_t*)a.out + ((size_t)p.i * a.q_heads + head0 + r) * a.head_dim;
+#pragma unroll
+        for (int j = 0; j < HD / 16; ++j) {
+            const float* o = acc.o[g][j];
+            uint32_t w0, w1;
+            if (a.q_dt == AQ_F16) {
+                w0 = round_pack2<AQ_F16>(o[0] * inv[0], o[1] * inv[1]);
+                w1 = round_pack2<AQ_F16>(o[2] * inv[0], o[3] * inv[1]);
+            } else {
+                w0 = round_pack2<AQ_BF16>(o[0] * inv[0], o[1] * inv[1]);
+                w1 = round_pack2<AQ_BF16>(o[2] * inv[0], o[3] * inv[1]);
+            }
+            w0 = transpose8x8(w0);
+            w1 = transpose8x8(w1);
+            if (r < rows && 16 * j < a.head_dim) {
+                if constexpr (DT == AQ_E4M3) {
+                    *(uint2*)(out + 16 * j + 4 * q) = make_uint2(prmt(w0, w1, 0x5410), prmt(w0, w1, 0x7632));
+                } else {
+                    *(uint32_t*)(out + 16 * j + 2 * q) = w0;
+                    *(uint32_t*)(out + 16 * j + 8 + 2 * q) = w1;
                 }
-            } else {
-                const int col = column_of<DT>(j, 0, q);
-                if (col < a.head_dim) store_out2(a, q_row, col, acc.o[j][2 * h] * inv, acc.o[j][2 * h + 1] * inv);
             }
         }
     }
 }
 
-// A partial: max of the 16 rows, their sums, then o [16][HD]; rows past the real ones are left out.
-template <int DT, int HD>
-__device__ __forceinline__ void write_partial(const Args& a, int tile, const Acc<HD>& acc, float* dst, int lane) {
+// A partial: the rows' maxima, their sums, then o; rows past the real ones are left out.
+template <int DT, int HD, int NH>
+__device__ __forceinline__ void write_partial(const Args& a, int tile, const Acc<HD, NH>& acc, float* dst, int lane) {
+    using T = Tile<DT, HD, NH>;
     int head0, rows;
-    tile_rows(a, tile, &head0, &rows);
-    const int g = lane >> 2, q = lane & 3;
+    tile_rows<T::ROWS>(a, tile, &head0, &rows);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const float l = quad_sum(acc.l[h]);
-        const int r = g + 8 * h;
-        if (r >= rows) continue;
-        if (q == 0) dst[r] = acc.m[h], dst[16 + r] = l;
-        float* o = dst + 32 + r * HD;
+    for (int g = 0; g < NH; ++g)
 #pragma unroll
-        for (int j = 0; j < HD / 8; ++j) {
-            if constexpr (DT == AQ_E4M3) {
-                o[column_of<DT>(j, 0, q)] = acc.o[j][2 * h];
-                o[column_of<DT>(j, 1, q)] = acc.o[j][2 * h + 1];
-            } else {
-                *(float2*)(o + column_of<DT>(j, 0, q)) = make_float2(acc.o[j][2 * h], acc.o[j][2 * h + 1]);
+        for (int x = 0; x < 2; ++x) {
+            const float l = column_sum(acc.l[g][x]);
+            const int r = 8 * g + 2 * (lane & 3) + x;
+            if (r >= rows) continue;
+            if (lane < 4) dst[r] = acc.m[g][x], dst[T::ROWS + r] = l;
+            float* o = dst + 2 * T::ROWS + r * T::OS;
+#pragma unroll
+            for (int j = 0; j < HD / 16; ++j) {
+                o[dim_of<DT>(j, 0, lane)] = acc.o[g][j][x];
+                o[dim_of<DT>(j, 1, lane)] = acc.o[g][j][2 + x];
             }
         }
-    }
 }
 
 // The factor that brings a partial with maximum m to maximum top.
 __device__ __forceinline__ float rebase(float m, float top) { return m == -INFINITY ? 0.0f : exp2_fast(m - top); }
 
-// The query tile as A fragments (rows = query heads, k = head dimension), in the order of k that
-// the keys' fragments come in, and each row's score factor: scale * log2 e, for E4M3 caches times
-// the power of two that the row was divided by to fit fp16.
-template <int DT, int HD>
-__device__ __forceinline__ void load_query(const Args& a, const Place& p, int lane, uint32_t (&qf)[HD / 16][4],
-                                           float (&factor)[2]) {
-    int head0, rows;
-    tile_rows(a, p.tile, &head0, &rows);
-    const int g = lane >> 2, q = lane & 3;
+// Loads that reach what other SMs wrote, and shared memory as well.
+__device__ __forceinline__ float ld_shared_or_l2(const float* p) {
+    float v;
+    asm volatile("ld.relaxed.gpu.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float4 ld4_shared_or_l2(const float* p) {
+    float4 v;
+    asm volatile("ld.relaxed.gpu.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    return v;
+}
+
+// Row r of the `count` <= 32 partials of the list put together by a warp, in order, to output row
+// q_row, or to the partial dst (which may be one of the list: a row is read and written by one
+// warp). A lane takes four columns. The one copy of this code serves the CTA's own pieces and the
+// joins, and is kept short: it runs once or twice in a call, and most of its time would go into
+// fetching instructions.
+template <int HD, int ROWS, int OS>
+__device__ __noinline__ void merge_row(const Args& a, const float* const* list, int count, int r, size_t q_row, float* dst) {
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY, l = 0.0f;
+    if (lane < count) {
+        const float* p = list[lane] + r;
+        m = ld_shared_or_l2(p), l = ld_shared_or_l2(p + ROWS);
+    }
+    float top = m;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = g + 8 * h;
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    const float f = rebase(m, top == -INFINITY ? 0.0f : top);
+    float sum = f * l;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    const float inv = inverse_sum(sum);
+    if (lane == 0) {
+        if (dst) dst[r] = top, dst[ROWS + r] = sum;
+        else if (a.lse) a.lse[q_row] = lse_of(top, sum);
+    }
+#pragma unroll 1
+    for (int c = 0; c < HD; c += 128) {
+        const int col = c + 4 * (HD < 128 ? lane & (HD / 4 - 1) : lane);
+        const int at = 2 * ROWS + r * OS + col;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+        for (int y0 = 0; y0 < count; y0 += 8) {
+            float4 v[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) v[y] = ld4_shared_or_l2(list[min(y0 + y, count - 1)] + at);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float fy = __shfl_sync(~0u, f, y0 + y);
+                if (y0 + y < count) o.x += fy * v[y].x, o.y += fy * v[y].y, o.z += fy * v[y].z, o.w += fy * v[y].w;
+            }
+        }
+        if (dst) {
+            *(float4*)(dst + at) = o;
+        } else if (col < a.head_dim) {
+            store_out2(a, q_row, col, o.x * inv, o.y * inv);
+            store_out2(a, q_row, col + 2, o.z * inv, o.w * inv);
+        }
+    }
+}
+
+// Adds 1 to a counter; what the CTA wrote before (and a barrier) is seen by whoever counts next.
+__device__ __forceinline__ int count_arrival(int* n) {
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(n) : "memory");
+    return old;
+}
+
+// The query tile as B fragments (columns = query heads, k = head dimension), in the order of k that
+// the keys' fragments come in, and each column's score factor: scale * log2 e, for E4M3 caches
+// times the power of two that the row was divided by to fit fp16.
+template <int DT, int HD, int NH>
+__device__ __forceinline__ void load_query(const Args& a, const Place& p, int lane, uint32_t (&qf)[NH][HD / 16][2],
+                                           float (&factor)[NH][2]) {
+    int head0, rows;
+    tile_rows<8 * NH>(a, p.tile, &head0, &rows);
+    const int q = lane & 3;
+#pragma unroll
+    for (int g = 0; g < NH; ++g) {
+        const int r = 8 * g + (lane >> 2);
+        const bool real = r < rows;
         const uint16_t* row = (const uint16_t*)a.q + (size_t)p.i * a.q_stride + (size_t)(head0 + r) * a.head_dim;
-        factor[h] = a.scale * kLog2e;
+        factor[g][0] = factor[g][1] = a.scale * kLog2e;
         if constexpr (DT != AQ_E4M3) {
 #pragma unroll
             for (int ks = 0; ks < HD / 16; ++ks)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int col = 16 * ks + 8 * x + 2 * q;
-                    qf[ks][2 * x + h] = r < rows && col < a.head_dim ? *(const uint32_t*)(row + col) : 0u;
-                }
+                for (int x = 0; x < 2; ++x)
+                    qf[g][ks][x] = real && 16 * ks < a.head_dim ? *(const uint32_t*)(row + 16 * ks + 8 * x + 2 * q) : 0u;
         } else {
             uint2 w[HD / 16];
             float top = 0.0f;
 #pragma unroll
+            for (int ks = 0; ks < HD / 16; ++ks)
+                w[ks] = real && 16 * ks < a.head_dim ? *(const uint2*)(row + 16 * ks + 4 * q) : make_uint2(0, 0);
+            auto widen = [&](const uint2& v, float (&f)[4]) {
+                if (a.q_dt == AQ_F16) widen2<AQ_F16>(v.x, f[0], f[1]), widen2<AQ_F16>(v.y, f[2], f[3]);
+                else widen2<AQ_BF16>(v.x, f[0], f[1]), widen2<AQ_BF16>(v.y, f[2], f[3]);
+            };
+#pragma unroll
             for (int ks = 0; ks < HD / 16; ++ks) {
-                const int col = 16 * ks + 4 * q;
-                w[ks] = r < rows && col < a.head_dim ? *(const uint2*)(row + col) : make_uint2(0, 0);
                 float f[4];
-                if (a.q_dt == AQ_F16) widen2<AQ_F16>(w[ks].x, f[0], f[1]), widen2<AQ_F16>(w[ks].y, f[2], f[3]);
-                else widen2<AQ_BF16>(w[ks].x, f[0], f[1]), widen2<AQ_BF16>(w[ks].y, f[2], f[3]);
+                widen(w[ks], f);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(f[x]));
             }
-            top = quad_max(top);
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
             const int e = min(max(exponent_of(top) - 14, -126), 112);    // |q| 2^-e < 2^15
-            const float down = pow2f(-e);
-            factor[h] *= pow2f(e);
+            const float down = pow2f(-e), up = pow2f(e);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) factor[g][x] *= __shfl_sync(~0u, up, 4 * (2 * q + x));
 #pragma unroll
             for (int ks = 0; ks < HD / 16; ++ks) {
                 float f[4];
-                if (a.q_dt == AQ_F16) widen2<AQ_F16>(w[ks].x, f[0], f[1]), widen2<AQ_F16>(w[ks].y, f[2], f[3]);
-                else widen2<AQ_BF16>(w[ks].x, f[0], f[1]), widen2<AQ_BF16>(w[ks].y, f[2], f[3]);
-                qf[ks][h] = round_pack2<AQ_F16>(f[0] * down, f[1] * down);
-                qf[ks][2 + h] = round_pack2<AQ_F16>(f[2] * down, f[3] * down);
+                widen(w[ks], f);
+                qf[g][ks][0] = round_pack2<AQ_F16>(f[0] * down, f[1] * down);
+                qf[g][ks][1] = round_pack2<AQ_F16>(f[2] * down, f[3] * down);
             }
         }
     }
@@ -346,15 +465,17 @@ __device__ __forceinline__ void load_query(const Args& a, const Place& p, int la
 // token's page. cur/nxt hold 32 table entries each, one a lane, from entry 32 * block on.
 template <int DT, int HD>
 struct Loader {
-    using T = Tile<DT, HD>;
-    int cur, nxt, block;
+    using T = Tile<DT, HD, 1>;
+    int cur, nxt, block, seq;
 
     __device__ __forceinline__ int entry(const Args& a, const Place& p, int b, int lane) const {
         const long long e = (long long)b * 32 + lane;
         return e << a.page_log2 < p.len ? a.tables[(size_t)p.seq * a.max_pages + e] : -1;
     }
     __device__ __forceinline__ void begin(const Args& a, const Place& p, int lane) {
-        block = (p.t >> a.page_log2) >> 5;
+        const int b = (p.t >> a.page_log2) >> 5;
+        if (p.seq == seq && b == block) return;        // the next head of a short sequence
+        block = b, seq = p.seq;
         cur = entry(a, p, block, lane);
         nxt = entry(a, p, block + 1, lane);
     }
@@ -367,23 +488,36 @@ struct Loader {
         }
         const int kvh = p.tile / a.tiles_per_head;
         const int mask = (1 << a.page_log2) - 1;
-        constexpr int RPP = 32 / (T::PR < 32 ? T::PR : 32);      // rows per pass
         static_assert(T::PR <= 32, "a row is at most 32 pieces");
+        constexpr int RPP = 32 / T::PR;                          // rows per pass
         const int piece = lane % T::PR, row0 = lane / T::PR;
         const bool real = piece * 16 < a.head_dim * T::ESZ;
         const size_t row_bytes = (size_t)a.head_dim * T::ESZ;
+        const int first = __shfl_sync(~0u, cur, e0 & 31);
+        if (mask >= T::CT - 1 && p.t + T::CT <= p.len && (unsigned)first < (unsigned)a.num_pages) {
+            // all of the chunk is cached, in one page: its rows follow one another
+            const size_t off = (((((size_t)first * a.kv_heads + kvh) << a.page_log2) + (p.t & mask) + row0) * row_bytes) +
+                               (real ? piece * 16 : 0);
+            const uint8_t *k = a.k + off, *v = a.v + off;
 #pragma unroll
-        for (int r0 = 0; r0 < T::CT; r0 += RPP) {
-            const int r = r0 + row0, tok = p.t + r;
-            const int page = __shfl_sync(~0u, cur, (tok >> a.page_log2) & 31);
-            const bool in = tok < p.len;
-            const bool ok = in && (unsigned)page < (unsigned)a.num_pages;
-            if (in && !ok) record_status(a.status, AQ_ERR_INVALID_ARG);
-            const size_t at = ok ? (((size_t)page * a.kv_heads + kvh) << a.page_log2) + (tok & mask) : 0;
-            const size_t off = ok && real ? at * row_bytes + piece * 16 : 0;
-            const uint32_t d = stage + swz<T::PR>(r, piece);
-            cp16(d, a.k + off, ok && real);
-            cp16(d + T::KV, a.v + off, ok && real);
+            for (int r0 = 0; r0 < T::CT; r0 += RPP) {
+                const uint32_t d = stage + swz<T::PR>(r0 + row0, piece);
+                cp16(d, k + r0 * row_bytes, real);
+                cp16(d + T::KV, v + r0 * row_bytes, real);
+            }
+        } else {
+#pragma unroll 1
+            for (int r = row0; r < T::CT; r += RPP) {
+                const int tok = p.t + r;
+                const int page = __shfl_sync(~0u, cur, (tok >> a.page_log2) & 31);
+                const bool in = tok < p.len, ok = in && (unsigned)page < (unsigned)a.num_pages;
+                if (in && !ok) record_status(a.status, AQ_ERR_INVALID_ARG);
+                const size_t at = ok ? (((size_t)page * a.kv_heads + kvh) << a.page_log2) + (tok & mask) : 0;
+                const size_t off = ok && real ? at * row_bytes + piece * 16 : 0;
+                const uint32_t d = stage + swz<T::PR>(r, piece);
+                cp16(d, a.k + off, ok && real);
+                cp16(d + T::KV, a.v + off, ok && real);
+            }
         }
         if constexpr (DT == AQ_E4M3) {
             // scale bytes, four tokens (of one page) a lane: keys' at 2 KV, values' at 2 KV + 64
@@ -400,144 +534,148 @@ struct Loader {
 };
 
 // One chunk: scores, running maximum and sum, output.
-template <int DT, int HD>
-__device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane, const uint32_t (&qf)[HD / 16][4],
-                                        const float (&factor)[2], Acc<HD>& acc) {
-    using T = Tile<DT, HD>;
+template <int DT, int HD, int NH>
+__device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane, const uint32_t (&qf)[NH][HD / 16][2],
+                                        const float (&factor)[NH][2], Acc<HD, NH>& acc) {
+    using T = Tile<DT, HD, NH>;
     constexpr bool BF = DT == AQ_BF16;
-    constexpr int NT = T::CT / 8;
-    const int q = lane & 3;
+    constexpr int TT = T::CT / 16;                 // tiles of 16 tokens
+    const int row = lane >> 2;                     // tokens of this lane in a tile: row and row + 8
     const int mi = lane >> 3, mr = lane & 7;       // this lane's matrix and row in an ldmatrix.x4
-    float s[NT][4];
+    float s[TT][NH][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int g = 0; g < NH; ++g) s[tt][g][0] = s[tt][g][1] = s[tt][g][2] = s[tt][g][3] = 0.0f;
     if constexpr (DT != AQ_E4M3) {
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks)
 #pragma unroll
-            for (int tt = 0; tt < NT / 2; ++tt) {
-                uint32_t b[4];
-                ldsm4(stage + swz<T::PR>(tt * 16 + (mi >> 1) * 8 + mr, 2 * ks + (mi & 1)), b);
-                mma16816<BF>(s[2 * tt], qf[ks], b[0], b[1]);
-                mma16816<BF>(s[2 * tt + 1], qf[ks], b[2], b[3]);
+            for (int tt = 0; tt < TT; ++tt) {
+                uint32_t k[4];
+                ldsm4(stage + swz<T::PR>(tt * 16 + (mi & 1) * 8 + mr, 2 * ks + (mi >> 1)), k);
+#pragma unroll
+                for (int g = 0; g < NH; ++g) mma16816<BF>(s[tt][g], k, qf[g][ks][0], qf[g][ks][1]);
             }
     } else {
 #pragma unroll
         for (int c = 0; c < HD / 16; c += 2)
 #pragma unroll
-            for (int tt = 0; tt < NT / 2; ++tt) {
-                uint32_t b[4];
-                ldsm4(stage + swz<T::PR>(tt * 16 + (mi & 1) * 8 + mr, c + (mi >> 1)), b);
+            for (int tt = 0; tt < TT; ++tt) {
+                uint32_t r[4];
+                ldsm4(stage + swz<T::PR>(tt * 16 + (mi & 1) * 8 + mr, c + (mi >> 1)), r);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    mma16816<false>(s[2 * tt], qf[c + x], widen_e4m3x2(b[2 * x]), widen_e4m3x2(b[2 * x] >> 16));
-                    mma16816<false>(s[2 * tt + 1], qf[c + x], widen_e4m3x2(b[2 * x + 1]),
-                                    widen_e4m3x2(b[2 * x + 1] >> 16));
+                    const uint32_t lo = r[2 * x], hi = r[2 * x + 1];
+                    const uint32_t k[4] = {widen_e4m3x2(lo), widen_e4m3x2(hi), widen_e4m3x2(lo >> 16),
+                                           widen_e4m3x2(hi >> 16)};
+#pragma unroll
+                    for (int g = 0; g < NH; ++g) mma16816<false>(s[tt][g], k, qf[g][c + x][0], qf[g][c + x][1]);
                 }
             }
     }
     // base-2 scores; masked ones are -inf
     const bool edge = p.t < p.lo || p.t + T::CT > p.len;
-    float vexp[NT][2], vfac[NT][2];               // b and 2^b of the tokens' value scales
+    float vexp[TT][2], vfac[TT][2];                // b and 2^b of the tokens' value scales
+    float top[NH][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        float kf[2] = {1.0f, 1.0f};
-        if constexpr (DT == AQ_E4M3) {
-            uint16_t kb, wb;
-            const uint32_t at = stage + 2 * T::KV + nt * 8 + 2 * q;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(kb) : "r"(at) : "memory");
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(wb) : "r"(at + 64) : "memory");
-            kf[0] = __uint_as_float((uint32_t)(kb & 255) << 23);
-            kf[1] = __uint_as_float((uint32_t)(kb >> 8) << 23);
-            vexp[nt][0] = (float)((int)(wb & 255) - 127);
-            vexp[nt][1] = (float)((int)(wb >> 8) - 127);
-            vfac[nt][0] = __uint_as_float((uint32_t)(wb & 255) << 23);
-            vfac[nt][1] = __uint_as_float((uint32_t)(wb >> 8) << 23);
-        }
+    for (int g = 0; g < NH; ++g) top[g][0] = top[g][1] = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int tok = p.t + nt * 8 + 2 * q + x;
+    for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float kf = 1.0f;
+            if constexpr (DT == AQ_E4M3) {
+                uint32_t kb, vb;
+                const uint32_t at = stage + 2 * T::KV + tt * 16 + h * 8 + row;
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(kb) : "r"(at) : "memory");
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vb) : "r"(at + 64) : "memory");
+                kf = __uint_as_float(kb << 23);
+                vexp[tt][h] = (float)((int)vb - 127);
+                vfac[tt][h] = __uint_as_float(vb << 23);
+            }
+            const int tok = p.t + tt * 16 + h * 8 + row;
             const bool out = edge && (tok < p.lo || tok >= p.len);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float v = s[nt][2 * h + x] * (DT == AQ_E4M3 ? factor[h] * kf[x] : factor[h]);
-                s[nt][2 * h + x] = out ? -INFINITY : v;
-            }
+            for (int g = 0; g < NH; ++g)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    float& v = s[tt][g][2 * h + x];
+                    v = out ? -INFINITY : v * (DT == AQ_E4M3 ? factor[g][x] * kf : factor[g][x]);
+                    top[g][x] = fmaxf(top[g][x], DT == AQ_E4M3 ? v + vexp[tt][h] : v);
+                }
         }
-    }
-    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                top[h] = fmaxf(top[h], DT == AQ_E4M3 ? s[nt][2 * h + x] + vexp[nt][x] : s[nt][2 * h + x]);
-    float sub[2];
+    float sub[NH][2];
     bool moved = false;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        top[h] = fmaxf(quad_max(top[h]), acc.m[h]);
-        moved |= top[h] > acc.m[h];
-        sub[h] = top[h] == -INFINITY ? 0.0f : top[h];
-    }
+    for (int g = 0; g < NH; ++g)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            top[g][x] = fmaxf(column_max(top[g][x]), acc.m[g][x]);
+            moved |= top[g][x] > acc.m[g][x];
+            sub[g][x] = top[g][x] == -INFINITY ? 0.0f : top[g][x];
+        }
     if (__any_sync(~0u, moved)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float f = rebase(acc.m[h], sub[h]);
-            acc.m[h] = top[h];
-            acc.l[h] *= f;
+        for (int g = 0; g < NH; ++g)
 #pragma unroll
-            for (int j = 0; j < HD / 8; ++j) acc.o[j][2 * h] *= f, acc.o[j][2 * h + 1] *= f;
-        }
+            for (int x = 0; x < 2; ++x) {
+                const float f = rebase(acc.m[g][x], sub[g][x]);
+                acc.m[g][x] = top[g][x];
+                acc.l[g][x] *= f;
+#pragma unroll
+                for (int j = 0; j < HD / 16; ++j) acc.o[g][j][x] *= f, acc.o[g][j][2 + x] *= f;
+            }
     }
-    // weights: p for the sum, p 2^b rounded to 16 bits for the product with V
-    uint32_t w[NT][2];                              // [token tile][row half]
+    // weights: p for the sum, p 2^b rounded to 16 bits for the product with V, as B fragments
+    uint32_t w[TT][NH][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float p0 = exp2_fast(s[nt][2 * h] - sub[h]), p1 = exp2_fast(s[nt][2 * h + 1] - sub[h]);
-            acc.l[h] += p0 + p1;
-            if constexpr (DT == AQ_E4M3) p0 *= vfac[nt][0], p1 *= vfac[nt][1];
-            w[nt][h] = round_pack2<BF ? AQ_BF16 : AQ_F16>(p0, p1);
-        }
+        for (int g = 0; g < NH; ++g)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float p0 = exp2_fast(s[tt][g][2 * h] - sub[g][0]), p1 = exp2_fast(s[tt][g][2 * h + 1] - sub[g][1]);
+                acc.l[g][0] += p0;
+                acc.l[g][1] += p1;
+                if constexpr (DT == AQ_E4M3) p0 *= vfac[tt][h], p1 *= vfac[tt][h];
+                w[tt][g][h] = transpose8x8(round_pack2<BF ? AQ_BF16 : AQ_F16>(p0, p1));
+            }
     const uint32_t vt = stage + T::KV;
 #pragma unroll
-    for (int kt = 0; kt < NT / 2; ++kt) {
-        const uint32_t a[4] = {w[2 * kt][0], w[2 * kt][1], w[2 * kt + 1][0], w[2 * kt + 1][1]};
+    for (int tt = 0; tt < TT; ++tt) {
         if constexpr (DT != AQ_E4M3) {
 #pragma unroll
-            for (int jp = 0; jp < HD / 16; ++jp) {
-                uint32_t b[4];
-                ldsm4t(vt + swz<T::PR>(kt * 16 + (mi & 1) * 8 + mr, 2 * jp + (mi >> 1)), b);
-                mma16816<BF>(acc.o[2 * jp], a, b[0], b[1]);
-                mma16816<BF>(acc.o[2 * jp + 1], a, b[2], b[3]);
+            for (int j = 0; j < HD / 16; ++j) {
+                uint32_t v[4];
+                ldsm4t(vt + swz<T::PR>(tt * 16 + (mi >> 1) * 8 + mr, 2 * j + (mi & 1)), v);
+#pragma unroll
+                for (int g = 0; g < NH; ++g) mma16816<BF>(acc.o[g][j], v, w[tt][g][0], w[tt][g][1]);
             }
         } else {
 #pragma unroll
             for (int c = 0; c < HD / 16; c += 2) {
-                uint32_t b[4];
-                ldsm4t(vt + swz<T::PR>(kt * 16 + (mi & 1) * 8 + mr, c + (mi >> 1)), b);
+                uint32_t r[4];
+                ldsm4t(vt + swz<T::PR>(tt * 16 + (mi & 1) * 8 + mr, c + (mi >> 1)), r);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const uint32_t lo = b[2 * x], hi = b[2 * x + 1];   // tokens 2q, 2q+1; +8
-                    mma16816<false>(acc.o[2 * (c + x)], a, widen_e4m3x2(prmt(lo, 0, 0x20)),
-                                    widen_e4m3x2(prmt(hi, 0, 0x20)));
-                    mma16816<false>(acc.o[2 * (c + x) + 1], a, widen_e4m3x2(prmt(lo, 0, 0x31)),
-                                    widen_e4m3x2(prmt(hi, 0, 0x31)));
+                    const uint32_t lo = r[2 * x], hi = r[2 * x + 1];   // tokens 2q, 2q+1; + 8
+                    const uint32_t v[4] = {widen_e4m3x2(prmt(lo, 0, 0x20)), widen_e4m3x2(prmt(lo, 0, 0x31)),
+                                           widen_e4m3x2(prmt(hi, 0, 0x20)), widen_e4m3x2(prmt(hi, 0, 0x31))};
+#pragma unroll
+                    for (int g = 0; g < NH; ++g) mma16816<false>(acc.o[g][c + x], v, w[tt][g][0], w[tt][g][1]);
                 }
             }
         }
     }
 }
 
-// Chunk offsets of the launch's n entries into base[0..n] (shared), their ranges and sequences;
+// Positions of the launch's n entries into base[0..n] (shared), their ranges and sequences;
 // all threads. Each thread takes consecutive entries, so the sums stay in order.
-template <int CT>
+template <int CT, int WARPS>
 __device__ void scan_entries(const Args& a, int tiles, long long* base, int2* range, int* seq_of) {
-    __shared__ long long warp_sum[kWarps];
-    constexpr int PER = kSliceSeqs / kThreads;
+    __shared__ long long warp_sum[WARPS];
+    constexpr int PER = kSliceSeqs / (32 * WARPS);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long c[PER], mine = 0;
 #pragma unroll
@@ -549,7 +687,8 @@ __device__ void scan_entries(const Args& a, int tiles, long long* base, int2* ra
             seq_range(a, i, &seq, &len, &lo, blockIdx.x == 0);
             range[i] = make_int2(len, lo);
             seq_of[i] = seq;
-            c[j] = (long long)chunks_of<CT>(len, lo) * tiles;
+            const int chunks = chunks_of<CT>(len, lo);
+            c[j] = chunks ? (long long)(chunks + SEG) * tiles : 0;
         }
         mine += c[j];
     }
@@ -573,28 +712,146 @@ __device__ void scan_entries(const Args& a, int tiles, long long* base, int2* ra
     __syncthreads();
 }
 
-// Chunks each warp takes.
-__device__ __forceinline__ long long share_of(long long total, int ctas) {
-    const long long warps = (long long)ctas * kWarps;
-    const long long per = (total + warps - 1) / warps;
+// Positions each warp takes.
+__device__ __forceinline__ long long share_of(long long total, int warps) {
+    const long long per = quotient(total + warps - 1, warps);
     return per < 1 ? 1 : per;
 }
 
-template <int DT, int HD>
-__global__ void __launch_bounds__(kThreads, (Tile<DT, HD>::CTAS)) kv_attend_kernel(Args a) {
-    using T = Tile<DT, HD>;
+// A segment that crosses CTAs: the first of them, how many they are, its query rows.
+struct Crossing {
+    int j0, count, rows;
+    size_t q_row;
+    // CTAs that are joined at a time, and the first of CTA k's group.
+    __device__ __forceinline__ int group() const { return count <= 32 ? count : 16; }
+    __device__ __forceinline__ int first_of(int k) const { return count <= 32 ? 0 : k & ~15; }
+};
+
+template <int WARPS>
+struct Shared {
+    long long base[kSliceSeqs + 1];   // positions of the entries' first segments
+    int2 range[kSliceSeqs];           // their lengths and first tokens seen
+    int seq_of[kSliceSeqs];
+    int piece_seg[2 * WARPS];         // segments of the warps' first and last pieces (-1: none)
+    const float* list[WARPS][32];     // the partials that a warp puts together
+    Crossing cross[2];
+    bool last[2];
+};
+
+// What the CTA does after its warps' shares: merges their pieces, and joins what crosses CTAs if
+// it is the last of them.
+template <int DT, int HD, int NH>
+__device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::WARPS>& s, const uint8_t* ring, long long share,
+                                    long long cta0, long long cta1) {
+    using T = Tile<DT, HD, NH>;
+    constexpr int kWarps = T::WARPS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tiles = a.kv_heads * a.tiles_per_head;
+    const float* const first = a.first + (size_t)(blockIdx.x * kWarps) * T::PART;
+    // Pieces of the CTA's warps, in order (lane y holds piece y's segment); those of one segment
+    // are adjacent. Warps take the segments' rows in turn. At most two segments cross the CTA's
+    // ends; what there is of them becomes partials (0: of the one that began before, 1: of the one
+    // that begins here).
+    const float** const list = s.list[warp];
+    const int mine = lane < 2 * kWarps ? s.piece_seg[lane] : -1;
+    int crossing = 0, turn = 0;
+#pragma unroll 1
+    for (unsigned rest = __ballot_sync(~0u, mine >= 0); rest;) {
+        const int seg = __shfl_sync(~0u, mine, __ffs(rest) - 1);
+        const unsigned of_seg = __ballot_sync(~0u, mine == seg);
+        rest &= ~of_seg;
+        const int i = seg / tiles, tile = seg - i * tiles;
+        const long long per = chunks_of<T::CT>(s.range[i].x, s.range[i].y) + SEG;
+        const long long s0 = s.base[i] + per * tile + SEG, s1 = s.base[i] + per * (tile + 1);
+        const bool done = s0 >= cta0 && s1 <= cta1;
+        const int which = s0 < cta0 ? 0 : 1;
+        int head0, rows;
+        tile_rows<T::ROWS>(a, tile, &head0, &rows);
+        if (!done) {
+            crossing |= 1 << which;
+            if (threadIdx.x == which) {
+                Crossing& x = s.cross[which];
+                x.j0 = (int)quotient(s0, share * kWarps);
+                x.count = (int)quotient(s1 - 1, share * kWarps) - x.j0 + 1;
+                x.rows = rows;
+                x.q_row = (size_t)i * a.q_heads + head0;
+            }
+        }
+        if (of_seg >> lane & 1)
+            list[__popc(of_seg & ((1u << lane) - 1))] =
+                lane & 1 ? (const float*)(ring + (lane >> 1) * T::RING) : first + (lane >> 1) * T::PART;
+        __syncwarp();
+        float* const dst = done ? nullptr : a.part + ((size_t)blockIdx.x * 2 + which) * T::PART;
+        for (int r = (warp - turn) & (kWarps - 1); r < rows; r += kWarps)
+            merge_row<HD, T::ROWS, T::OS>(a, list, __popc(of_seg), r, (size_t)i * a.q_heads + head0 + r, dst);
+        __syncwarp();
+        turn += rows;
+    }
+    if (!crossing) return;
+
+    // Of the CTAs that hold a crossing segment, the last to get here joins it. Where there are many
+    // (few kv heads, one long sequence) groups of consecutive CTAs are joined first, in the same
+    // way, each into its first CTA's partial.
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        bool all = false;
+        if (crossing >> threadIdx.x & 1) {
+            const Crossing x = s.cross[threadIdx.x];
+            const int k0 = x.first_of((int)blockIdx.x - x.j0);
+            int* n = a.arrived + 2 * (x.j0 + k0) + (k0 == 0 ? 1 : 0);
+            all = count_arrival(n) == min(x.group(), x.count - k0) - 1;
+            if (all) *n = 0;                       // for the next call
+        }
+        s.last[threadIdx.x] = all;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int w = 0; w < 2; ++w) {
+        if (!s.last[w]) continue;
+        const Crossing x = s.cross[w];
+        const int g = x.group();
+        int k = x.first_of((int)blockIdx.x - x.j0), step = 1, members = min(g, x.count - k);
+        bool final = g == x.count;
+#pragma unroll 1
+        while (true) {
+            auto part = [&](int y) {
+                const int j = k + y * step;
+                return a.part + (size_t)((x.j0 + j) * 2 + (j == 0 ? 1 : 0)) * T::PART;
+            };
+            if (lane < members) list[lane] = part(lane);
+            __syncwarp();
+            for (int r = warp; r < x.rows; r += kWarps)
+                merge_row<HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, final ? nullptr : part(0));
+            __syncwarp();
+            if (final) break;
+            members = (x.count + g - 1) / g, step = g, k = 0, final = true;   // the groups' results
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                int* n = a.arrived + 2 * kMaxCtas + x.j0;
+                s.last[w] = count_arrival(n) == members - 1;
+                if (s.last[w]) *n = 0;
+            }
+            __syncthreads();
+            if (!s.last[w]) break;
+        }
+    }
+}
+
+template <int DT, int HD, int NH>
+__global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(const __grid_constant__ Args a) {
+    using T = Tile<DT, HD, NH>;
+    constexpr int kWarps = T::WARPS, kThreads = T::THREADS;
     extern __shared__ __align__(1024) uint8_t ring[];
-    __shared__ long long base[kSliceSeqs + 1];
-    __shared__ int2 range[kSliceSeqs];
-    __shared__ int seq_of[kSliceSeqs];
-    __shared__ long long piece_seg[kWarps][2];     // the segments of a warp's first and last piece
+    __shared__ Shared<kWarps> s;
+    long long* const base = s.base;
+    int2* const range = s.range;
+    int* const seq_of = s.seq_of;
+    int* const piece_seg = s.piece_seg;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = a.kv_heads * a.tiles_per_head;
     pdl_wait();
-    scan_entries<T::CT>(a, tiles, base, range, seq_of);
+    scan_entries<T::CT, kWarps>(a, tiles, base, range, seq_of);
     pdl_launch_dependents();
-    if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i <= a.n; i += kThreads) a.base[i] = base[i];
     // entries that see nothing
     for (int i = blockIdx.x; i < a.n; i += gridDim.x)
         if (range[i].x <= 0) {
@@ -603,229 +860,102 @@ __global__ void __launch_bounds__(kThreads, (Tile<DT, HD>::CTAS)) kv_attend_kern
             if (a.lse)
                 for (int j = threadIdx.x; j < a.q_heads; j += kThreads) a.lse[(size_t)i * a.q_heads + j] = -INFINITY;
         }
-    const long long total = base[a.n], share = share_of(total, gridDim.x);
+    const long long total = base[a.n], share = share_of(total, gridDim.x * kWarps);
     const long long cta0 = min(total, share * kWarps * blockIdx.x), cta1 = min(total, cta0 + share * kWarps);
     const long long u0 = min(total, cta0 + share * warp), u1 = min(total, u0 + share);
     if (cta0 >= cta1) return;
 
-    float* slots[2] = {a.first + (size_t)(blockIdx.x * kWarps + warp) * T::PART,
-                       (float*)(ring + warp * T::RING)};
-    if (lane == 0) piece_seg[warp][0] = piece_seg[warp][1] = -1;
+    float* const first = a.first + (size_t)(blockIdx.x * kWarps) * T::PART;    // first pieces: global
+    if (lane < 2) piece_seg[2 * warp + lane] = -1;
     __syncwarp();
-    if (u0 < u1) {
+    Place at;
+    if (u0 < u1) place_at<T::CT>(a, base, range, seq_of, u0, at);
+    if (u0 < u1 && at.pos < u1) {
         const uint32_t stages = smem_u32(ring + warp * T::RING);
-        Place in, at;
-        place_at<T::CT>(a, base, range, seq_of, tiles, u0, in);
-        at = in;
+        Place in = at;
+        bool more = true;                          // chunk `in` is still to be issued
         Loader<DT, HD> loader;
+        loader.seq = -1;
         loader.begin(a, in, lane);
-        const int count = (int)(u1 - u0);
-        int issued = 0, fill = 0;
+        int fill = 0;
         auto issue = [&]() {
-            if (issued < count) {
+            if (more) {
                 loader.issue(a, in, stages + fill * T::STAGE, lane);
-                if (++issued < count && advance<T::CT>(a, range, seq_of, tiles, in)) loader.begin(a, in, lane);
+                more = next_pos(in) < u1;
+                if (more && advance<T::CT>(a, range, seq_of, tiles, in)) loader.begin(a, in, lane);
             }
             if (++fill == T::NS) fill = 0;
             cp_async_commit();
         };
-        uint32_t qf[HD / 16][4];
-        float factor[2];
-        Acc<HD> acc;
+        uint32_t qf[NH][HD / 16][2];
+        float factor[NH][2];
+        Acc<HD, NH> acc;
         bool whole = at.t / T::CT == at.lo / T::CT;   // the segment begins in this warp's share
-        load_query<DT, HD>(a, at, lane, qf, factor);
-        acc.clear();
 #pragma unroll 1
         for (int k = 0; k < T::NS - 1; ++k) issue();
+        load_query<DT, HD, NH>(a, at, lane, qf, factor);
+        acc.clear();
         int use = 0;
 #pragma unroll 1
-        for (int k = 0; k < count; ++k) {
+        while (true) {
             issue();
             cp_async_wait<T::NS - 1>();
             __syncwarp();
-            compute<DT, HD>(at, stages + use * T::STAGE, lane, qf, factor, acc);
+            compute<DT, HD, NH>(at, stages + use * T::STAGE, lane, qf, factor, acc);
             __syncwarp();
             if (++use == T::NS) use = 0;
-            const bool last = k + 1 == count;
-            if (at.left == 1 || last) {
-                const long long seg = (long long)at.i * tiles + at.tile;
-                if (whole && at.left == 1) {
-                    write_final<DT, HD>(a, at, acc, lane);
-                } else if (!last) {
-                    write_partial<DT, HD>(a, at.tile, acc, slots[0], lane);
-                    if (lane == 0) piece_seg[warp][0] = seg;
-                } else {
-                    cp_async_wait<0>();            // (nothing but empty groups is left)
-                    __syncwarp();
-                    write_partial<DT, HD>(a, at.tile, acc, slots[1], lane);
-                    if (lane == 0) piece_seg[warp][1] = seg;
-                }
-                if (!last) {
-                    advance<T::CT>(a, range, seq_of, tiles, at);
-                    whole = true;
-                    load_query<DT, HD>(a, at, lane, qf, factor);
-                    acc.clear();
-                }
-            } else {
+            const bool last = next_pos(at) >= u1, ends = at.left == 1;
+            if (!last && !ends) {
                 at.t += T::CT;
                 --at.left;
+                ++at.pos;
+                continue;
             }
+            if (whole && ends) {
+                write_final<DT, HD, NH>(a, at, acc, lane);
+            } else {
+                // The ring is free once the share's last chunk has been read (only empty groups
+                // of copies are left then); earlier pieces go to global memory.
+                float* dst = last ? (float*)(ring + warp * T::RING) : first + warp * T::PART;
+                write_partial<DT, HD, NH>(a, at.tile, acc, dst, lane);
+                if (lane == 0) piece_seg[2 * warp + last] = at.i * tiles + at.tile;
+            }
+            if (last) break;
+            advance<T::CT>(a, range, seq_of, tiles, at);
+            whole = true;
+            load_query<DT, HD, NH>(a, at, lane, qf, factor);
+            acc.clear();
         }
     }
     __syncthreads();
-
-    // Pieces of the CTA's warps, in order; those of one segment are adjacent.
-    const float* piece[2 * kWarps];
-    long long seg[2 * kWarps];
-    int pieces = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (piece_seg[w][x] >= 0) {
-                seg[pieces] = piece_seg[w][x];
-                piece[pieces++] = x == 0 ? a.first + (size_t)(blockIdx.x * kWarps + w) * T::PART
-                                         : (const float*)(ring + w * T::RING);
-            }
-    for (int b = 0; b < pieces;) {
-        int e = b + 1;
-        while (e < pieces && seg[e] == seg[b]) ++e;
-        const int i = (int)(seg[b] / tiles), tile = (int)(seg[b] - (long long)i * tiles);
-        const long long per = chunks_of<T::CT>(range[i].x, range[i].y);
-        const long long s0 = base[i] + per * tile, s1 = s0 + per;
-        const bool done = s0 >= cta0 && s1 <= cta1;
-        float* dst = a.part + ((size_t)blockIdx.x * 2 + (s0 < cta0 ? 0 : 1)) * T::PART;
-        int head0, rows;
-        tile_rows(a, tile, &head0, &rows);
-        for (int x = threadIdx.x; x < rows * (HD / 4); x += kThreads) {
-            const int r = x / (HD / 4), col = (x - r * (HD / 4)) * 4;
-            float top = -INFINITY;
-            for (int y = b; y < e; ++y) top = fmaxf(top, piece[y][r]);
-            const float sub = top == -INFINITY ? 0.0f : top;
-            float l = 0.0f;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int y = b; y < e; ++y) {
-                const float f = rebase(piece[y][r], sub);
-                const float4 v = *(const float4*)(piece[y] + 32 + r * HD + col);
-                l += f * piece[y][16 + r];
-                o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
-            }
-            if (done) {
-                const size_t q_row = (size_t)i * a.q_heads + head0 + r;
-                const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-                if (col < a.head_dim) {
-                    store_out2(a, q_row, col, o.x * inv, o.y * inv);
-                    store_out2(a, q_row, col + 2, o.z * inv, o.w * inv);
-                }
-                if (a.lse && col == 0) a.lse[q_row] = l == l ? lse_of(top, l) : l;
-            } else {
-                if (col == 0) dst[r] = top, dst[16 + r] = l;
-                *(float4*)(dst + 32 + r * HD + col) = o;
-            }
-        }
-        b = e;
-    }
+    finish<DT, HD, NH>(a, s, ring, share, cta0, cta1);
 }
 
-// Joins the segments that cross CTAs of the kernel above. CTA (j, y) takes the segment that
-// crosses the end of CTA j's share and began in it, rows y, y + gridDim.y, ...; the partials are
-// summed by groups of HD / 4 threads, in a fixed order.
-template <int DT, int HD>
-__global__ void __launch_bounds__(kThreads) kv_join_kernel(Args a, int ctas) {
-    using T = Tile<DT, HD>;
-    constexpr int LANES = HD / 4, GROUPS = kThreads / LANES;
-    __shared__ float red_m[kWarps], red_l[GROUPS];
-    __shared__ float4 red_o[GROUPS][LANES];
-    pdl_wait();
-    const int tiles = a.kv_heads * a.tiles_per_head;
-    const long long total = a.base[a.n], share = share_of(total, ctas) * kWarps;
-    const long long end = share * (blockIdx.x + 1);
-    if (end >= total) return;
-    int lo = 0, hi = a.n - 1;                      // the entry of chunk end - 1
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.base[mid] <= end - 1) lo = mid;
-        else hi = mid - 1;
-    }
-    const long long b0 = a.base[lo], per = (a.base[lo + 1] - b0) / tiles;
-    const int tile = (int)((end - 1 - b0) / per);
-    const long long s0 = b0 + per * tile, s1 = s0 + per;
-    if (s1 == end || s0 < end - share) return;     // not crossing, or begun before
-    const int j0 = blockIdx.x, j1 = (int)((s1 - 1) / share);
-    int head0, rows;
-    tile_rows(a, tile, &head0, &rows);
-    const int sub = threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
-    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        auto part = [&](int j) { return a.part + ((size_t)j * 2 + (j == j0 ? 1 : 0)) * T::PART; };
-        float top = -INFINITY;
-        for (int j = j0 + threadIdx.x; j <= j1; j += kThreads) top = fmaxf(top, part(j)[r]);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        if ((threadIdx.x & 31) == 0) red_m[threadIdx.x >> 5] = top;
-        __syncthreads();
-        top = red_m[0];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, red_m[w]);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float l = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int j = j0 + sub; j <= j1; j += GROUPS) {
-            const float* p = part(j);
-            const float f = rebase(p[r], ref);
-            const float4 v = *(const float4*)(p + 32 + r * HD + col);
-            l += f * p[16 + r];
-            o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
-        }
-        red_o[sub][col / 4] = o;
-        if (col == 0) red_l[sub] = l;
-        __syncthreads();
-        if (sub == 0) {
-            for (int g = 1; g < GROUPS; ++g) {
-                const float4 v = red_o[g][col / 4];
-                l += red_l[g];
-                o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
-            }
-            const size_t q_row = (size_t)lo * a.q_heads + head0 + r;
-            const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-            if (col < a.head_dim) {
-                store_out2(a, q_row, col, o.x * inv, o.y * inv);
-                store_out2(a, q_row, col + 2, o.z * inv, o.w * inv);
-            }
-            if (a.lse && col == 0) a.lse[q_row] = l == l ? lse_of(top, l) : l;
-        }
-        __syncthreads();
-    }
-}
-
-// The workspace is sized for the largest grid, so that the query needs no device.
-constexpr int kMaxSms = 160;
-
-template <int DT, int HD>
+template <int DT, int HD, int NH>
 size_t attend_ws() {
-    return kWsStatusBytes + round_up((kSliceSeqs + 1) * 8, 256) +
-           (size_t)kMaxSms * Tile<DT, HD>::CTAS * (2 + kWarps) * Tile<DT, HD>::PART * 4;
+    using T = Tile<DT, HD, NH>;
+    return kWsStatusBytes + kArrivedBytes + (size_t)kMaxCtas * (2 + T::WARPS) * T::PART * 4;
 }
 
-template <int DT, int HD>
+template <int DT, int HD, int NH>
 aq_status attend(Args a, const DeviceInfo& di, int n, cudaStream_t st) {
-    using T = Tile<DT, HD>;
+    using T = Tile<DT, HD, NH>;
     static std::atomic<bool> have[64];             // (setting the attribute twice is harmless)
     int dev = 0;
     if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
     if (!have[dev & 63]) {
-        if (cudaError_t e = cudaFuncSetAttribute(kv_attend_kernel<DT, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 T::SMEM);
+        if (cudaError_t e = cudaFuncSetAttribute(kv_attend_kernel<DT, HD, NH>,
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
             e != cudaSuccess)
             return cuda_fail(e, "cudaFuncSetAttribute");
         have[dev & 63] = true;
     }
-    const int ctas = (di.sms < kMaxSms ? di.sms : kMaxSms) * T::CTAS;
+    const int ctas = di.sms < kMaxCtas ? di.sms : kMaxCtas;
     char* ws = (char*)a.status;
-    a.base = (long long*)(ws + kWsStatusBytes);
-    a.part = (float*)(ws + kWsStatusBytes + round_up((kSliceSeqs + 1) * 8, 256));
+    a.arrived = (int*)(ws + kWsStatusBytes);
+    a.part = (float*)(ws + kWsStatusBytes + kArrivedBytes);
     a.first = a.part + (size_t)ctas * 2 * T::PART;
-    const int tiles = a.kv_heads * a.tiles_per_head, rows = a.group < 16 ? a.group : 16;
+    a.tiles_per_head = (a.group + T::ROWS - 1) / T::ROWS;
     for (int i0 = 0; i0 < n; i0 += kSliceSeqs) {
         Args s = a;
         s.n = n - i0 < kSliceSeqs ? n - i0 : kSliceSeqs;
@@ -834,31 +964,28 @@ aq_status attend(Args a, const DeviceInfo& di, int n, cudaStream_t st) {
         s.q = (const uint16_t*)a.q + (size_t)i0 * a.q_stride;
         s.out = (uint16_t*)a.out + (size_t)i0 * a.q_heads * a.head_dim;
         if (s.lse) s.lse += (size_t)i0 * a.q_heads;
-        if (aq_status e = launch_dependent(kv_attend_kernel<DT, HD>, ctas, kThreads, T::SMEM, st, s); e != AQ_OK)
+        if (aq_status e = launch_dependent(kv_attend_kernel<DT, HD, NH>, ctas, T::THREADS, T::SMEM, st, s); e != AQ_OK)
             return e;
-        // With few segments each is cut into many partials, and its rows get a CTA each.
-        const dim3 grid(ctas - 1, (long long)s.n * tiles < ctas ? rows : 1);
-        if (aq_status e = launch_dependent(kv_join_kernel<DT, HD>, grid, kThreads, 0, st, s, ctas); e != AQ_OK) return e;
     }
     return AQ_OK;
 }
 
-// Calls f<DT, HD>() for the cache's type and padded head dimension.
-#define AQ_KV_DISPATCH(dtype, dim, f, ...)                                            \
-    (dim) <= 64    ? ((dtype) == AQ_F16    ? f<AQ_F16, 64>(__VA_ARGS__)               \
-                      : (dtype) == AQ_BF16 ? f<AQ_BF16, 64>(__VA_ARGS__)              \
-                                           : f<AQ_E4M3, 64>(__VA_ARGS__))             \
-    : (dim) <= 128 ? ((dtype) == AQ_F16    ? f<AQ_F16, 128>(__VA_ARGS__)              \
-                      : (dtype) == AQ_BF16 ? f<AQ_BF16, 128>(__VA_ARGS__)             \
-                                           : f<AQ_E4M3, 128>(__VA_ARGS__))            \
-                   : ((dtype) == AQ_F16    ? f<AQ_F16, 256>(__VA_ARGS__)              \
-                      : (dtype) == AQ_BF16 ? f<AQ_BF16, 256>(__VA_ARGS__)             \
-                                           : f<AQ_E4M3, 256>(__VA_ARGS__))
+// Calls f<DT, HD, NH>() for the cache's type, the padded head dimension and one or two groups of
+// eight query heads per tile.
+#define AQ_KV_DISPATCH_HD(HD, f, ...)                                                       \
+    (c.dtype == AQ_F16    ? (two ? f<AQ_F16, HD, 2>(__VA_ARGS__) : f<AQ_F16, HD, 1>(__VA_ARGS__))   \
+     : c.dtype == AQ_BF16 ? (two ? f<AQ_BF16, HD, 2>(__VA_ARGS__) : f<AQ_BF16, HD, 1>(__VA_ARGS__)) \
+                          : (two ? f<AQ_E4M3, HD, 2>(__VA_ARGS__) : f<AQ_E4M3, HD, 1>(__VA_ARGS__)))
+#define AQ_KV_DISPATCH(f, ...)                                  \
+    (c.head_dim <= 64    ? AQ_KV_DISPATCH_HD(64, f, __VA_ARGS__)  \
+     : c.head_dim <= 128 ? AQ_KV_DISPATCH_HD(128, f, __VA_ARGS__) \
+                         : AQ_KV_DISPATCH_HD(256, f, __VA_ARGS__))
 
 }  // namespace
 
-size_t kv_attend_ws_bytes(const aq_kv_cache& c) {
-    return AQ_KV_DISPATCH(c.dtype, c.head_dim, attend_ws);
+size_t kv_attend_ws_bytes(const aq_kv_cache& c, int q_heads) {
+    const bool two = q_heads / c.kv_heads > 8;
+    return AQ_KV_DISPATCH(attend_ws);
 }
 
 aq_status launch_kv_attend(const aq_kv_cache& c, const DeviceInfo& di, int layer, int n, const int* seqs,
@@ -879,11 +1006,11 @@ aq_status launch_kv_attend(const aq_kv_cache& c, const DeviceInfo& di, int layer
     a.status = (unsigned int*)ws;
     a.scale = scale;
     a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads / c.kv_heads;
-    a.tiles_per_head = (a.group + 15) / 16;
     a.head_dim = c.head_dim;
     while ((1 << a.page_log2) < c.page_tokens) ++a.page_log2;
     a.num_pages = c.num_pages, a.max_seqs = c.max_seqs, a.max_pages = c.max_pages, a.window = window;
-    return AQ_KV_DISPATCH(c.dtype, c.head_dim, attend, a, di, n, st);
+    const bool two = a.group > 8;
+    return AQ_KV_DISPATCH(attend, a, di, n, st);
 }
 
 }  // namespace aq
