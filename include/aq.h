@@ -424,7 +424,7 @@ typedef struct aq_kv_cache {
     int32_t layers;         /* >= 1 */
     int32_t num_pages;      /* pages of the pool, >= 1 */
     int32_t page_tokens;    /* a power of two, 8..1024 */
-    int32_t kv_heads;       /* >= 1 */
+    int32_t kv_heads;       /* 1..16384 */
     int32_t head_dim;       /* a multiple of 16, 16..256 */
     int32_t max_seqs;       /* sequence slots, >= 1 */
     int32_t max_pages;      /* entries of a sequence's table, >= 1 (max_pages * page_tokens < 2^31) */

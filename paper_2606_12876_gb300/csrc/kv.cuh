@@ -39,6 +39,29 @@ __device__ __forceinline__ void load8(const void* p, size_t i, int dt, float (&f
         else unpack8<AQ_BF16>(v, f);
     }
 }
+// Eight elements as loaded, 16 or 32 bytes (WIDE: fp32), and their widening, apart from each other
+// so that a run of loads is not broken by a branch on the type (dt is the same for all threads).
+template <bool WIDE>
+struct Raw {
+    uint4 v[WIDE ? 2 : 1];
+    __device__ __forceinline__ void load(const void* p, size_t i) {
+        const uint4* q = (const uint4*)((const char*)p + i * (WIDE ? 4 : 2));
+        v[0] = q[0];
+        if constexpr (WIDE) v[1] = q[1];
+    }
+    __device__ __forceinline__ void widen(int dt, float (&f)[8]) const {
+        if constexpr (WIDE) {
+            const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+        } else if (dt == AQ_F16) {
+            unpack8<AQ_F16>(v[0], f);
+        } else {
+            unpack8<AQ_BF16>(v[0], f);
+        }
+    }
+};
+
 __device__ __forceinline__ void store8(void* p, size_t i, int dt, const float (&f)[8]) {
     if (dt == AQ_F32) {
         float4* q = (float4*)((float*)p + i);

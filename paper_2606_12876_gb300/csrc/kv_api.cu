@@ -18,7 +18,7 @@ aq_status check_cache(const aq_kv_cache* c) {
     if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)))
         return AQ_ERR_UNSUPPORTED;
     if (c->head_dim % 16 || c->head_dim > 256) return AQ_ERR_UNSUPPORTED;
-    if ((long long)c->max_pages * c->page_tokens > INT_MAX || c->kv_heads > 65535) return AQ_ERR_UNSUPPORTED;
+    if ((long long)c->max_pages * c->page_tokens > INT_MAX || c->kv_heads > 16384) return AQ_ERR_UNSUPPORTED;
     return AQ_OK;
 }
 

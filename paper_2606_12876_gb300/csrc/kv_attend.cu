@@ -58,7 +58,7 @@ struct Tile {
     static constexpr int ROWS = 8 * NH;                      // query heads of a tile
     static constexpr int OS = HD + 4;                        // floats from one row of a partial's o to the next
     static constexpr int PART = 2 * ROWS + ROWS * OS;        // floats of a partial: maxima, sums, o
-    static_assert(RING >= PART * 4, "a warp's ring holds its last partial");
+    static_assert(RING >= 2 * PART * 4 && PART % 4 == 0, "a warp's ring holds its two pieces at the end");
     static constexpr int WARPS = HD == 256 ? 4 : 8;
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int SMEM = WARPS * RING;
@@ -337,31 +337,26 @@ __device__ __forceinline__ void write_partial(const Args& a, int tile, const Acc
 // The factor that brings a partial with maximum m to maximum top.
 __device__ __forceinline__ float rebase(float m, float top) { return m == -INFINITY ? 0.0f : exp2_fast(m - top); }
 
-// Loads that reach what other SMs wrote, and shared memory as well.
-__device__ __forceinline__ float ld_shared_or_l2(const float* p) {
-    float v;
-    asm volatile("ld.relaxed.gpu.f32 %0, [%1];" : "=f"(v) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ float4 ld4_shared_or_l2(const float* p) {
-    float4 v;
-    asm volatile("ld.relaxed.gpu.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
-    return v;
-}
-
 // Row r of the `count` <= 32 partials of the list put together by a warp, in order, to output row
 // q_row, or to the partial dst (which may be one of the list: a row is read and written by one
-// warp). A lane takes four columns. The one copy of this code serves the CTA's own pieces and the
-// joins, and is kept short: it runs once or twice in a call, and most of its time would go into
-// fetching instructions.
-template <int HD, int ROWS, int OS>
+// warp). A lane takes four columns, BATCH partials are under way at a time. OWN: the CTA's own
+// pieces, in shared memory; otherwise partials of other CTAs, read through L2. Out of line: the
+// main loop keeps its registers to itself.
+template <bool OWN, int BATCH, int HD, int ROWS, int OS>
 __device__ __noinline__ void merge_row(const Args& a, const float* const* list, int count, int r, size_t q_row, float* dst) {
     const int lane = threadIdx.x & 31;
-    float m = -INFINITY, l = 0.0f;
-    if (lane < count) {
-        const float* p = list[lane] + r;
-        m = ld_shared_or_l2(p), l = ld_shared_or_l2(p + ROWS);
-    }
+    auto load = [](const float* q) { return OWN ? *q : __ldcg(q); };
+    auto load4 = [](const float* q) { return OWN ? *(const float4*)q : __ldcg((const float4*)q); };
+    const float* p = list[min(lane, count - 1)] + r;
+    float m = load(p), l = load(p + ROWS);
+    float4 v[BATCH];
+    auto fetch = [&](int at, int y0) {               // (past the end: the last one again)
+#pragma unroll
+        for (int y = 0; y < BATCH; ++y) v[y] = load4(list[min(y0 + y, count - 1)] + at);
+    };
+    const int col0 = 4 * (HD < 128 ? lane & (HD / 4 - 1) : lane), at0 = 2 * ROWS + r * OS + col0;
+    fetch(at0, 0);                                   // before the maxima are known
+    if (lane >= count) m = -INFINITY, l = 0.0f;
     float top = m;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
@@ -376,19 +371,19 @@ __device__ __noinline__ void merge_row(const Args& a, const float* const* list, 
     }
 #pragma unroll 1
     for (int c = 0; c < HD; c += 128) {
-        const int col = c + 4 * (HD < 128 ? lane & (HD / 4 - 1) : lane);
-        const int at = 2 * ROWS + r * OS + col;
+        const int col = c + col0, at = at0 + c;
+        if (c > 0) fetch(at, 0);
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-        for (int y0 = 0; y0 < count; y0 += 8) {
-            float4 v[8];
+        for (int y0 = 0;;) {
 #pragma unroll
-            for (int y = 0; y < 8; ++y) v[y] = ld4_shared_or_l2(list[min(y0 + y, count - 1)] + at);
-#pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                const float fy = __shfl_sync(~0u, f, y0 + y);
+            for (int y = 0; y < BATCH; ++y) {
+                const float fy = __shfl_sync(~0u, f, (y0 + y) & 31);
                 if (y0 + y < count) o.x += fy * v[y].x, o.y += fy * v[y].y, o.z += fy * v[y].z, o.w += fy * v[y].w;
             }
+            y0 += BATCH;
+            if (y0 >= count) break;
+            fetch(at, y0);
         }
         if (dst) {
             *(float4*)(dst + at) = o;
@@ -399,7 +394,7 @@ __device__ __noinline__ void merge_row(const Args& a, const float* const* list, 
     }
 }
 
-// Adds 1 to a counter; what the CTA wrote before (and a barrier) is seen by whoever counts next.
+// Adds 1 to a counter; what the CTA wrote before (and a barrier) is seen by those that count later.
 __device__ __forceinline__ int count_arrival(int* n) {
     int old;
     asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(old) : "l"(n) : "memory");
@@ -489,7 +484,7 @@ struct Loader {
         const int kvh = p.tile / a.tiles_per_head;
         const int mask = (1 << a.page_log2) - 1;
         static_assert(T::PR <= 32, "a row is at most 32 pieces");
-        constexpr int RPP = 32 / T::PR;                          // rows per pass
+        constexpr int RPP = 32 / T::PR;                          // rows per pass, at most 8
         const int piece = lane % T::PR, row0 = lane / T::PR;
         const bool real = piece * 16 < a.head_dim * T::ESZ;
         const size_t row_bytes = (size_t)a.head_dim * T::ESZ;
@@ -504,6 +499,21 @@ struct Loader {
                 const uint32_t d = stage + swz<T::PR>(r0 + row0, piece);
                 cp16(d, k + r0 * row_bytes, real);
                 cp16(d + T::KV, v + r0 * row_bytes, real);
+            }
+        } else if (p.t + T::CT <= p.len) {
+            // all cached, in several pages (or a bad one): a pass of at most eight rows has one
+#pragma unroll
+            for (int r0 = 0; r0 < T::CT; r0 += RPP) {
+                const int page = __shfl_sync(~0u, cur, ((p.t + r0) >> a.page_log2) & 31);
+                const bool ok = (unsigned)page < (unsigned)a.num_pages;
+                if (!ok) record_status(a.status, AQ_ERR_INVALID_ARG);
+                const size_t off =
+                    ok && real ? ((((size_t)page * a.kv_heads + kvh) << a.page_log2) + ((p.t + r0) & mask) + row0) * row_bytes +
+                                     piece * 16
+                               : 0;
+                const uint32_t d = stage + swz<T::PR>(r0 + row0, piece);
+                cp16(d, a.k + off, ok && real);
+                cp16(d + T::KV, a.v + off, ok && real);
             }
         } else {
 #pragma unroll 1
@@ -738,72 +748,81 @@ struct Shared {
     bool last[2];
 };
 
-// What the CTA does after its warps' shares: merges their pieces, and joins what crosses CTAs if
-// it is the last of them.
+// What the CTA does after its warps' shares. Pieces of one segment are adjacent; the warps take the
+// segments' rows in turn and merge their pieces. Of a segment that crosses CTAs (at most two of a
+// CTA's do) that gives a partial (0: of the one that began before, 1: of the one that begins here),
+// which come first: the segments that are the CTA's own are merged while its arrival is counted
+// (a fence and an atomic through L2, one of each per CTA). The last CTA of a crossing segment to
+// arrive joins the partials. Where there are many (few kv heads, one long sequence) groups of
+// consecutive CTAs are joined first, in the same way, each into its first CTA's partial.
 template <int DT, int HD, int NH>
 __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::WARPS>& s, const uint8_t* ring, long long share,
-                                    long long cta0, long long cta1) {
+                                       long long cta0, long long cta1) {
     using T = Tile<DT, HD, NH>;
     constexpr int kWarps = T::WARPS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = a.kv_heads * a.tiles_per_head;
-    const float* const first = a.first + (size_t)(blockIdx.x * kWarps) * T::PART;
-    // Pieces of the CTA's warps, in order (lane y holds piece y's segment); those of one segment
-    // are adjacent. Warps take the segments' rows in turn. At most two segments cross the CTA's
-    // ends; what there is of them becomes partials (0: of the one that began before, 1: of the one
-    // that begins here).
     const float** const list = s.list[warp];
+    // Lane y holds piece y's segment: its rows, whether all of it is here, and if not its place
+    // among the CTA's two crossing segments, its first CTA and how many it crosses.
     const int mine = lane < 2 * kWarps ? s.piece_seg[lane] : -1;
-    int crossing = 0, turn = 0;
-#pragma unroll 1
-    for (unsigned rest = __ballot_sync(~0u, mine >= 0); rest;) {
-        const int seg = __shfl_sync(~0u, mine, __ffs(rest) - 1);
-        const unsigned of_seg = __ballot_sync(~0u, mine == seg);
-        rest &= ~of_seg;
-        const int i = seg / tiles, tile = seg - i * tiles;
-        const long long per = chunks_of<T::CT>(s.range[i].x, s.range[i].y) + SEG;
-        const long long s0 = s.base[i] + per * tile + SEG, s1 = s.base[i] + per * (tile + 1);
-        const bool done = s0 >= cta0 && s1 <= cta1;
-        const int which = s0 < cta0 ? 0 : 1;
-        int head0, rows;
+    const unsigned pieces = __ballot_sync(~0u, mine >= 0);
+    int head0 = 0, rows = 0, entry = 0, j0 = 0, ctas = 0, which = 0;
+    bool done = false;
+    if (mine >= 0) {
+        entry = mine / tiles;
+        const int tile = mine - entry * tiles;
+        const long long per = chunks_of<T::CT>(s.range[entry].x, s.range[entry].y) + SEG;
+        const long long s0 = s.base[entry] + per * tile + SEG, s1 = s.base[entry] + per * (tile + 1);
         tile_rows<T::ROWS>(a, tile, &head0, &rows);
+        done = s0 >= cta0 && s1 <= cta1;
+        which = s0 < cta0 ? 0 : 1;
         if (!done) {
-            crossing |= 1 << which;
-            if (threadIdx.x == which) {
-                Crossing& x = s.cross[which];
-                x.j0 = (int)quotient(s0, share * kWarps);
-                x.count = (int)quotient(s1 - 1, share * kWarps) - x.j0 + 1;
-                x.rows = rows;
-                x.q_row = (size_t)i * a.q_heads + head0;
+            j0 = (int)quotient(s0, share * kWarps);
+            ctas = (int)quotient(s1 - 1, share * kWarps) - j0 + 1;
+        }
+    }
+    const bool crossing = __any_sync(~0u, mine >= 0 && !done);
+    int turn = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        const unsigned of_pass = __ballot_sync(~0u, mine >= 0 && done == (pass == 1));
+#pragma unroll 1
+        for (unsigned rest = of_pass; rest;) {
+            const int y0 = __ffs(rest) - 1;
+            const unsigned of_seg = __ballot_sync(~0u, mine == __shfl_sync(~0u, mine, y0));
+            rest &= ~of_seg;
+            const int seg_rows = __shfl_sync(~0u, rows, y0);
+            int r = (warp - turn) & (kWarps - 1);
+            turn += seg_rows;
+            const size_t q_row = (size_t)__shfl_sync(~0u, entry, y0) * a.q_heads + __shfl_sync(~0u, head0, y0);
+            const int w = __shfl_sync(~0u, which, y0);
+            if (pass == 0 && threadIdx.x == y0) s.cross[w] = {j0, ctas, rows, q_row};
+            if (r >= seg_rows) continue;
+            if (of_seg >> lane & 1)
+                list[__popc(of_seg & ((1u << lane) - 1))] = (const float*)(ring + (lane >> 1) * T::RING) + (lane & 1) * T::PART;
+            __syncwarp();
+            float* const dst = pass == 1 ? nullptr : a.part + ((size_t)blockIdx.x * 2 + w) * T::PART;
+            for (; r < seg_rows; r += kWarps)
+                merge_row<true, 4, HD, T::ROWS, T::OS>(a, list, __popc(of_seg), r, q_row + r, dst);
+            __syncwarp();
+        }
+        if (pass == 0 && crossing) {
+            __syncthreads();
+            if (threadIdx.x < 2) {
+                bool all = false;
+                const Crossing x = s.cross[threadIdx.x];
+                if (x.count > 0) {
+                    const int k0 = x.first_of((int)blockIdx.x - x.j0);
+                    int* n = a.arrived + 2 * (x.j0 + k0) + (k0 == 0 ? 1 : 0);
+                    all = count_arrival(n) == min(x.group(), x.count - k0) - 1;
+                    if (all) *n = 0;               // for the next call
+                }
+                s.last[threadIdx.x] = all;
             }
         }
-        if (of_seg >> lane & 1)
-            list[__popc(of_seg & ((1u << lane) - 1))] =
-                lane & 1 ? (const float*)(ring + (lane >> 1) * T::RING) : first + (lane >> 1) * T::PART;
-        __syncwarp();
-        float* const dst = done ? nullptr : a.part + ((size_t)blockIdx.x * 2 + which) * T::PART;
-        for (int r = (warp - turn) & (kWarps - 1); r < rows; r += kWarps)
-            merge_row<HD, T::ROWS, T::OS>(a, list, __popc(of_seg), r, (size_t)i * a.q_heads + head0 + r, dst);
-        __syncwarp();
-        turn += rows;
     }
     if (!crossing) return;
-
-    // Of the CTAs that hold a crossing segment, the last to get here joins it. Where there are many
-    // (few kv heads, one long sequence) groups of consecutive CTAs are joined first, in the same
-    // way, each into its first CTA's partial.
-    __syncthreads();
-    if (threadIdx.x < 2) {
-        bool all = false;
-        if (crossing >> threadIdx.x & 1) {
-            const Crossing x = s.cross[threadIdx.x];
-            const int k0 = x.first_of((int)blockIdx.x - x.j0);
-            int* n = a.arrived + 2 * (x.j0 + k0) + (k0 == 0 ? 1 : 0);
-            all = count_arrival(n) == min(x.group(), x.count - k0) - 1;
-            if (all) *n = 0;                       // for the next call
-        }
-        s.last[threadIdx.x] = all;
-    }
     __syncthreads();
 #pragma unroll 1
     for (int w = 0; w < 2; ++w) {
@@ -820,8 +839,11 @@ __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::W
             };
             if (lane < members) list[lane] = part(lane);
             __syncwarp();
-            for (int r = warp; r < x.rows; r += kWarps)
-                merge_row<HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, final ? nullptr : part(0));
+            float* const dst = final ? nullptr : part(0);
+            for (int r = warp; r < x.rows; r += kWarps) {
+                if (members <= 4) merge_row<false, 4, HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, dst);
+                else merge_row<false, 20, HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, dst);
+            }
             __syncwarp();
             if (final) break;
             members = (x.count + g - 1) / g, step = g, k = 0, final = true;   // the groups' results
@@ -867,6 +889,7 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
 
     float* const first = a.first + (size_t)(blockIdx.x * kWarps) * T::PART;    // first pieces: global
     if (lane < 2) piece_seg[2 * warp + lane] = -1;
+    if (threadIdx.x < 2) s.cross[threadIdx.x].count = 0;
     __syncwarp();
     Place at;
     if (u0 < u1) place_at<T::CT>(a, base, range, seq_of, u0, at);
@@ -915,8 +938,8 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
                 write_final<DT, HD, NH>(a, at, acc, lane);
             } else {
                 // The ring is free once the share's last chunk has been read (only empty groups
-                // of copies are left then); earlier pieces go to global memory.
-                float* dst = last ? (float*)(ring + warp * T::RING) : first + warp * T::PART;
+                // of copies are left then); an earlier piece waits in global memory.
+                float* dst = last ? (float*)(ring + warp * T::RING) + T::PART : first + warp * T::PART;
                 write_partial<DT, HD, NH>(a, at.tile, acc, dst, lane);
                 if (lane == 0) piece_seg[2 * warp + last] = at.i * tiles + at.tile;
             }
@@ -926,6 +949,14 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
             load_query<DT, HD, NH>(a, at, lane, qf, factor);
             acc.clear();
         }
+    }
+    __syncwarp();
+    if (piece_seg[2 * warp] >= 0) {                // the first piece, to where the ring was
+        const float* src = first + warp * T::PART;
+        const uint32_t dst = smem_u32(ring + warp * T::RING);
+        for (int x = lane; x < T::PART / 4; x += 32) cp16(dst + x * 16, src + x * 4, true);
+        cp_async_commit();
+        cp_async_wait<0>();
     }
     __syncthreads();
     finish<DT, HD, NH>(a, s, ring, share, cta0, cta1);

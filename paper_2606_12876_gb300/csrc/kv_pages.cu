@@ -9,8 +9,6 @@
 // every other decision is made in one CTA, so the outcome does not depend on scheduling. A page
 // shared by several sequences is always full (a fork copies a partial last page), so no write
 // ever needs to ask whether its page is shared.
-#include <climits>
-
 #include "kv.cuh"
 
 namespace aq {
@@ -23,51 +21,61 @@ constexpr int kCopyVecs = 4;           // 16-byte vectors a thread has in flight
 constexpr int kCopyBytes = kCopyThreads * kCopyVecs * 16;
 
 // Exclusive prefix sum of v over the CTA (kPlanThreads threads); *total gets the sum. Synchronises.
-__device__ int block_scan(int v, int* total) {
-    __shared__ int warp_sum[kPlanThreads / 32];
+template <typename T>
+__device__ T block_scan(T v, T* total) {
+    __shared__ T warp_sum[kPlanThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int s = v;
+    T s = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, s, d);
+        const T o = __shfl_up_sync(~0u, s, d);
         if (lane >= d) s += o;
     }
     if (lane == 31) warp_sum[warp] = s;
     __syncthreads();
-    int w = warp_sum[lane];                       // kPlanThreads / 32 == 32 warps
+    T w = warp_sum[lane];                         // kPlanThreads / 32 == 32 warps
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(~0u, w, d);
+        const T o = __shfl_up_sync(~0u, w, d);
         if (lane >= d) w += o;
     }
-    const int before = warp ? __shfl_sync(~0u, w, warp - 1) : 0;
+    const T before = __shfl_sync(~0u, w, warp ? warp - 1 : 0);
     *total = __shfl_sync(~0u, w, 31);
     __syncthreads();                              // warp_sum is written again by the next call
-    return before + s - v;
+    return (warp ? before : 0) + s - v;
 }
 
 __device__ __forceinline__ int pages_of(long long tokens, int page) { return (int)((tokens + page - 1) / page); }
 
-// The reference counts of pages [at, at + kPlanPages) (past the pool: -1).
-__device__ __forceinline__ void load_refs(const aq_kv_cache& c, int at, int (&r)[kPlanPages]) {
+// The reference counts of pages [at, at + kPlanPages) (past the pool: -1), at a multiple of four.
+__device__ __forceinline__ void load_refs(const aq_kv_cache& c, long long at, int (&r)[kPlanPages]) {
+    if (at + kPlanPages <= c.num_pages && ((uintptr_t)c.refs & 15) == 0) {
 #pragma unroll
-    for (int j = 0; j < kPlanPages; ++j) r[j] = at + j < c.num_pages ? c.refs[at + j] : -1;
+        for (int j = 0; j < kPlanPages; j += 4) {
+            const int4 v = *(const int4*)(c.refs + at + j);
+            r[j] = v.x, r[j + 1] = v.y, r[j + 2] = v.z, r[j + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPlanPages; ++j) r[j] = at + j < c.num_pages ? c.refs[at + j] : -1;
+    }
 }
 
 // The `total` lowest free pages into list, in order; returns how many there were (at most total).
-__device__ int find_free(const aq_kv_cache& c, int total, int* list) {
+// r: the counts of the first step, as load_refs gives them for this thread.
+__device__ int find_free(const aq_kv_cache& c, int total, int* list, int (&r)[kPlanPages]) {
     int found = 0;
-    for (int at = 0; at < c.num_pages && found < total; at += kPlanThreads * kPlanPages) {
-        int r[kPlanPages], mine = 0, all;
-        const int p0 = at + threadIdx.x * kPlanPages;
-        load_refs(c, p0, r);
+    for (long long at = 0; at < c.num_pages && found < total; at += kPlanThreads * kPlanPages) {
+        int mine = 0, all;
+        const long long p0 = at + threadIdx.x * kPlanPages;
+        if (at > 0) load_refs(c, p0, r);
 #pragma unroll
         for (int j = 0; j < kPlanPages; ++j) mine += r[j] == 0;
-        int rank = found + block_scan(mine, &all);
+        int rank = found + block_scan<int>(mine, &all);
 #pragma unroll
         for (int j = 0; j < kPlanPages; ++j)
             if (r[j] == 0) {
-                if (rank < total) list[rank] = p0 + j;
+                if (rank < total) list[rank] = (int)(p0 + j);
                 ++rank;
             }
         found += all;
@@ -79,67 +87,159 @@ __device__ int find_free(const aq_kv_cache& c, int total, int* list) {
 // Reserve (FORK = false): entry i lengthens sequence a[i] (i when a is null) by b[i] tokens (1 when
 // b is null). Fork (FORK = true): entry i makes the empty sequence b[i] a copy of a[i]; this
 // kernel plans it and allocates the copies of partial last pages, kv_share_kernel does the rest.
-// Nothing is changed unless every entry can be served. One CTA.
+// Nothing is changed unless every entry can be served. One CTA, up to kPlanThreads entries: a
+// thread has one, in registers. The time is that of dependent reads of the bookkeeping (entry,
+// length, last page; the reference counts are read meanwhile) and of a few barriers.
+struct Entry {
+    int from, seq, len, add, err;      // err: 0, or the status to record
+};
+template <bool FORK>
+__device__ __forceinline__ Entry load_entry(const aq_kv_cache& c, int i, const int* a, const int* b) {
+    Entry e;
+    e.from = a ? a[i] : i;
+    e.seq = FORK ? b[i] : e.from;
+    e.add = FORK ? 0 : b ? b[i] : 1;
+    e.len = 0, e.err = AQ_ERR_INVALID_ARG;
+    if ((unsigned)e.from < (unsigned)c.max_seqs && (unsigned)e.seq < (unsigned)c.max_seqs) {
+        e.len = c.lens[e.from];
+        const int taken = FORK ? c.lens[e.seq] : 0;
+        const long long len = (long long)e.len + e.add;
+        if (e.len >= 0 && e.add >= 0 && taken == 0)
+            e.err = len > (long long)c.max_pages * c.page_tokens ? AQ_ERR_CAPACITY : 0;
+    }
+    return e;
+}
+template <bool FORK>
+__device__ __forceinline__ int pages_needed(const aq_kv_cache& c, const Entry& e) {
+    return FORK ? e.len % c.page_tokens != 0
+                : pages_of((long long)e.len + e.add, c.page_tokens) - pages_of(e.len, c.page_tokens);
+}
+// The status of a whole call (an invalid entry before a lack of pages), for every thread.
+__device__ __forceinline__ int call_status(int err) {
+    if (__syncthreads_or(err == AQ_ERR_INVALID_ARG)) return AQ_ERR_INVALID_ARG;
+    return __syncthreads_or(err != 0) ? AQ_ERR_CAPACITY : 0;
+}
+
 template <bool FORK>
 __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(aq_kv_cache c, KvScratch s, int n, const int* a,
                                                                const int* b) {
-    __shared__ int bad;                           // the first error's status
+    constexpr int kSlots = 2 * kPlanThreads;
+    __shared__ int seen[kSlots];                  // the listed sequences + 1, hashed
+    __shared__ int list[kPlanThreads];            // allocated pages (more of them: s.dst)
+    __shared__ int prefix[kPlanThreads];          // pages of the entries before
+    __shared__ int first[kPlanThreads];           // reserve: an entry's sequence and its first new table entry
+    __shared__ int seqs[kPlanThreads];
     pdl_wait();
-    if (threadIdx.x == 0) bad = 0, s.ctl[0] = 0, s.ctl[1] = 0;
+    pdl_launch_dependents();
+    const int t = threadIdx.x;
+    seen[t] = seen[t + kPlanThreads] = 0;
+    int refs[kPlanPages];
+    load_refs(c, t * kPlanPages, refs);
+    Entry e = {0, 0, 0, 0, 0};
+    if (t < n) e = load_entry<FORK>(c, t, a, b);
+    const int need = t < n && e.err == 0 ? pages_needed<FORK>(c, e) : 0;
+    int old = 0;                                  // fork: the partial page
+    if (FORK && need) old = c.tables[(size_t)e.from * c.max_pages + e.len / c.page_tokens];
     __syncthreads();
-    const long long cap = (long long)c.max_pages * c.page_tokens;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-        const int from = a ? a[i] : i, seq = FORK ? b[i] : from;
-        int err = 0;
-        if ((unsigned)from >= (unsigned)c.max_seqs || (unsigned)seq >= (unsigned)c.max_seqs) {
-            err = AQ_ERR_INVALID_ARG;
-        } else {
-            const int len = c.lens[from], add = FORK ? 0 : b ? b[i] : 1;
-            if (len < 0 || add < 0 || (FORK && c.lens[seq] != 0)) err = AQ_ERR_INVALID_ARG;
-            else if ((long long)len + add > cap || (long long)len + add > INT_MAX) err = AQ_ERR_CAPACITY;
-            s.marks[seq] = i;
-            s.count[i] = len;
+    if (t < n && e.err != AQ_ERR_INVALID_ARG) {
+        for (unsigned h = (unsigned)e.seq * 2654435761u >> 21;; h = (h + 1) & (kSlots - 1)) {
+            const int was = atomicCAS(seen + h, 0, e.seq + 1);
+            if (was == e.seq + 1) e.err = AQ_ERR_INVALID_ARG;
+            if (was == 0 || was == e.seq + 1) break;
         }
-        if (err) atomicCAS(&bad, 0, err);
     }
-    __syncthreads();
-    // A sequence named twice keeps only one entry's mark. (Every thread has read `bad` before any
-    // thread writes it again: the branches around the CTA-wide steps are taken by all or none.)
-    int total = 0;
-    const bool valid = !bad;
-    __syncthreads();
-    if (valid) {
-        for (int at = 0; at < n; at += kPlanThreads) {
-            const int i = at + threadIdx.x;
-            int need = 0, all;
-            if (i < n) {
-                const int seq = FORK ? b[i] : a ? a[i] : i, len = s.count[i];
-                if (s.marks[seq] != i) atomicCAS(&bad, 0, AQ_ERR_INVALID_ARG);
-                need = FORK ? len % c.page_tokens != 0
-                            : pages_of((long long)len + (b ? b[i] : 1), c.page_tokens) - pages_of(len, c.page_tokens);
+    int status = call_status(e.err), total = 0, before = 0;
+    if (!status) {
+        long long all;                            // (may pass 32 bits)
+        before = (int)block_scan<long long>(need, &all);
+        if (all > c.num_pages) status = AQ_ERR_CAPACITY;
+        else total = (int)all;
+    }
+    int* const pages = total <= kPlanThreads ? list : s.dst;
+    if (!status && total > 0 && find_free(c, total, pages, refs) < total) status = AQ_ERR_CAPACITY;
+    if (t == 0) {
+        s.ctl[0] = status ? 0 : total, s.ctl[1] = !status;
+        if (status) record_status(s.status, status);
+    }
+    if (status) return;
+    if (FORK) {
+        if (t < n) {
+            if (need) {
+                const int page = list[before];
+                s.src[before] = old;
+                s.dst[before] = page;
+                c.tables[(size_t)e.seq * c.max_pages + e.len / c.page_tokens] = page;
+                c.refs[page] = 1;
             }
-            const int before = block_scan(need, &all);
-            if (i < n) s.prefix[i] = total + before;
-            if (all > INT_MAX - total) {          // (the same for every thread)
-                if (threadIdx.x == 0) atomicCAS(&bad, 0, AQ_ERR_CAPACITY);
-                break;
-            }
-            total += all;
+            s.count[t] = e.len;
+            c.lens[e.seq] = e.len;
         }
-        if (threadIdx.x == 0 && total > c.num_pages) atomicCAS(&bad, 0, AQ_ERR_CAPACITY);
-        __syncthreads();
-    }
-    const bool search = !bad && total > 0;
-    __syncthreads();
-    if (search) {
-        const int found = find_free(c, total, s.dst);
-        if (threadIdx.x == 0 && found < total) bad = AQ_ERR_CAPACITY;
-        __syncthreads();
-    }
-    if (bad) {
-        if (threadIdx.x == 0) record_status(s.status, bad);
         return;
     }
+    if (t < n) {
+        prefix[t] = before;
+        seqs[t] = e.seq;
+        first[t] = pages_of(e.len, c.page_tokens);
+        c.lens[e.seq] = e.len + e.add;
+    }
+    __syncthreads();
+    for (int k = t; k < total; k += kPlanThreads) {
+        int lo = 0, hi = n - 1;                   // the last entry whose prefix is <= k
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (prefix[mid] <= k) lo = mid;
+            else hi = mid - 1;
+        }
+        c.tables[(size_t)seqs[lo] * c.max_pages + first[lo] + k - prefix[lo]] = pages[k];
+        c.refs[pages[k]] = 1;
+    }
+}
+
+// The same for longer lists: what the one above keeps in registers and shared memory goes through
+// the workspace, kPlanThreads entries at a time.
+template <bool FORK>
+__global__ void __launch_bounds__(kPlanThreads) kv_plan_long_kernel(aq_kv_cache c, KvScratch s, int n, const int* a,
+                                                                    const int* b) {
+    pdl_wait();
+    pdl_launch_dependents();
+    int err = 0;
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const Entry e = load_entry<FORK>(c, i, a, b);
+        if (e.err != AQ_ERR_INVALID_ARG) s.marks[e.seq] = i;
+        s.count[i] = e.len;
+        if (err != AQ_ERR_INVALID_ARG && e.err) err = e.err;
+    }
+    int status = call_status(err), total = 0;
+    if (status != AQ_ERR_INVALID_ARG) {           // a sequence named twice keeps only one entry's mark
+        bool twice = false;
+        for (int i = threadIdx.x; i < n; i += kPlanThreads) twice |= s.marks[FORK ? b[i] : a ? a[i] : i] != i;
+        if (__syncthreads_or(twice)) status = AQ_ERR_INVALID_ARG;
+    }
+    for (int at = 0; at < n && !status; at += kPlanThreads) {
+        const int i = at + threadIdx.x;
+        int need = 0;
+        if (i < n) {
+            Entry e;
+            e.len = s.count[i], e.add = FORK ? 0 : b ? b[i] : 1;
+            need = pages_needed<FORK>(c, e);
+        }
+        long long all;
+        const long long before = block_scan<long long>(need, &all);
+        if (i < n) s.prefix[i] = (int)(total + before);
+        if (total + all > c.num_pages) status = AQ_ERR_CAPACITY;
+        else total += (int)all;
+    }
+    __syncthreads();
+    if (!status && total > 0) {
+        int refs[kPlanPages];
+        load_refs(c, threadIdx.x * kPlanPages, refs);
+        if (find_free(c, total, s.dst, refs) < total) status = AQ_ERR_CAPACITY;
+    }
+    if (threadIdx.x == 0) {
+        s.ctl[0] = status ? 0 : total, s.ctl[1] = !status;
+        if (status) record_status(s.status, status);
+    }
+    if (status) return;
     if (FORK) {
         for (int i = threadIdx.x; i < n; i += kPlanThreads) {
             const int len = s.count[i];
@@ -151,7 +251,6 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(aq_kv_cache c, Kv
             }
             c.lens[b[i]] = len;
         }
-        if (threadIdx.x == 0) s.ctl[0] = total, s.ctl[1] = 1;
     } else {
         for (int k = threadIdx.x; k < total; k += kPlanThreads) {
             int lo = 0, hi = n - 1;               // the last entry whose prefix is <= k
@@ -212,6 +311,7 @@ __device__ void copy_pages(const aq_kv_cache& c, int count, const int* src, cons
 __global__ void __launch_bounds__(kCopyThreads) kv_share_kernel(aq_kv_cache c, KvScratch s, int n, const int* src,
                                                                 const int* dst) {
     pdl_wait();
+    pdl_launch_dependents();
     if (!s.ctl[1]) return;
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
         const int full = s.count[i] / c.page_tokens;
@@ -230,6 +330,7 @@ __global__ void __launch_bounds__(kCopyThreads) kv_share_kernel(aq_kv_cache c, K
 __global__ void __launch_bounds__(kCopyThreads) kv_copy_kernel(aq_kv_cache c, unsigned int* status, int n,
                                                                const int* src, const int* dst) {
     pdl_wait();
+    pdl_launch_dependents();
     copy_pages(c, n, src, dst, status);
 }
 
@@ -238,6 +339,7 @@ __global__ void __launch_bounds__(kCopyThreads) kv_copy_kernel(aq_kv_cache c, un
 __global__ void __launch_bounds__(kCopyThreads) kv_free_kernel(aq_kv_cache c, unsigned int* status, const int* seqs) {
     __shared__ int shared_len;
     pdl_wait();
+    pdl_launch_dependents();
     const int seq = seqs ? seqs[blockIdx.x] : blockIdx.x;
     if ((unsigned)seq >= (unsigned)c.max_seqs) {
         if (threadIdx.x == 0) record_status(status, AQ_ERR_INVALID_ARG);
@@ -259,34 +361,36 @@ __global__ void __launch_bounds__(kCopyThreads) kv_free_kernel(aq_kv_cache c, un
 // page below U (there are equally many). One CTA.
 __global__ void __launch_bounds__(kPlanThreads) kv_compact_plan_kernel(aq_kv_cache c, KvScratch s, int* used_out) {
     pdl_wait();
+    pdl_launch_dependents();
     constexpr int kStep = kPlanThreads * kPlanPages;
-    int used = 0;
-    for (int at = 0; at < c.num_pages; at += kStep) {
-        int r[kPlanPages], mine = 0, all;
+    int used = 0, r[kPlanPages];
+    for (long long at = 0; at < c.num_pages; at += kStep) {
+        int mine = 0, all;
         load_refs(c, at + threadIdx.x * kPlanPages, r);
 #pragma unroll
         for (int j = 0; j < kPlanPages; ++j) mine += r[j] > 0;
-        block_scan(mine, &all);
+        block_scan<int>(mine, &all);
         used += all;
     }
     int holes = 0, movers = 0;
-    for (int at = 0; at < c.num_pages; at += kStep) {
-        int r[kPlanPages], hole = 0, mover = 0, all;
-        const int p0 = at + threadIdx.x * kPlanPages;
-        load_refs(c, p0, r);
+    for (long long at = 0; at < c.num_pages; at += kStep) {
+        int hole = 0, mover = 0, all;
+        const long long p0 = at + threadIdx.x * kPlanPages;
+        if (c.num_pages > kStep) load_refs(c, p0, r);          // (else they are still there)
 #pragma unroll
         for (int j = 0; j < kPlanPages; ++j) {
             hole += r[j] == 0 && p0 + j < used;
             mover += r[j] > 0 && p0 + j >= used;
         }
-        int h = holes + block_scan(hole, &all);
-        holes += all;
-        int m = movers + block_scan(mover, &all);
-        movers += all;
+        // both counts in one scan: a step has kStep < 2^16 pages
+        const int both = block_scan<int>(hole << 16 | mover, &all);
+        int h = holes + (int)((unsigned)both >> 16), m = movers + (both & 0xffff);
+        holes += (int)((unsigned)all >> 16);
+        movers += all & 0xffff;
 #pragma unroll
         for (int j = 0; j < kPlanPages; ++j) {
-            if (r[j] == 0 && p0 + j < used) s.dst[h++] = p0 + j;
-            if (r[j] > 0 && p0 + j >= used) s.src[m++] = p0 + j;
+            if (r[j] == 0 && p0 + j < used) s.dst[h++] = (int)(p0 + j);
+            if (r[j] > 0 && p0 + j >= used) s.src[m++] = (int)(p0 + j);
         }
     }
     __syncthreads();
@@ -307,6 +411,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_compact_plan_kernel(aq_kv_cac
 // Carries a compaction out: tables are rewritten, pages copied.
 __global__ void __launch_bounds__(kCopyThreads) kv_compact_kernel(aq_kv_cache c, KvScratch s) {
     pdl_wait();
+    pdl_launch_dependents();
     const int used = s.ctl[2], moves = s.ctl[0];
     if (moves == 0) return;
     for (int seq = blockIdx.x; seq < c.max_seqs; seq += gridDim.x) {
@@ -323,63 +428,96 @@ __global__ void __launch_bounds__(kCopyThreads) kv_compact_kernel(aq_kv_cache c,
 
 __global__ void __launch_bounds__(kCopyThreads) kv_init_kernel(aq_kv_cache c) {
     pdl_wait();
+    pdl_launch_dependents();
     const size_t t = (size_t)blockIdx.x * kCopyThreads + threadIdx.x, step = (size_t)gridDim.x * kCopyThreads;
     for (size_t i = t; i < (size_t)c.max_seqs * c.max_pages; i += step) c.tables[i] = -1;
     for (size_t i = t; i < (size_t)c.max_seqs; i += step) c.lens[i] = 0;
     for (size_t i = t; i < (size_t)c.num_pages; i += step) c.refs[i] = 0;
 }
 
-// New keys and values into their slots. A group of `lanes` lanes (a power of two, at least
-// head_dim / 8) takes one head of one token's key or value, eight elements a lane: one 16-byte
-// load and store each for 16-bit types; for E4M3 the group's maximum gives the scale.
+// New keys and values into their slots. A CTA takes a few tokens (one per group of `lanes` lanes, a
+// power of two that is at least head_dim / 8) and `heads` heads of their keys or of their values
+// (even and odd blockIdx.y); a lane takes eight elements of a row: one 16-byte load and store each
+// for 16-bit types; for E4M3 the group's maximum gives the scale. The tokens' slots are looked up
+// once, three dependent reads, while the first UNDER_WAY rows are under way. Bound by HBM for
+// prompts, by that chain for a decode step.
+template <int UNDER_WAY, bool WIDE>
 __global__ void __launch_bounds__(kCopyThreads) kv_write_kernel(aq_kv_cache c, int layer, int n, const int* seqs,
                                                                 const int* positions, const void* k, const void* v,
-                                                                int x_dt, long long stride, int lanes_log2,
+                                                                int x_dt, long long stride, int lanes_log2, int heads,
                                                                 unsigned int* status) {
+    __shared__ long long slots[kCopyThreads / 2];  // of the first head's row in the pool, or -1
     pdl_wait();
-    const int lane = threadIdx.x & ((1 << lanes_log2) - 1);
-    const int per_cta = kCopyThreads >> lanes_log2, slot0 = threadIdx.x >> lanes_log2;
-    const size_t rows = (size_t)n * 2 * c.kv_heads;
-    // Every thread makes the same number of trips: the shuffles below are warp-wide.
-    for (size_t base = (size_t)blockIdx.x * per_cta; base < rows; base += (size_t)gridDim.x * per_cta) {
-        const size_t r = base + slot0;
-        const bool in = r < rows && lane * 8 < c.head_dim;
-        const int head = (int)(r % c.kv_heads);
-        const size_t tr = r / c.kv_heads;
-        const int which = (int)(tr & 1);
-        const long long i = (long long)(tr >> 1);
-        float f[8] = {};
-        size_t at = 0;
-        bool ok = false;
-        if (r < rows) {
-            const int seq = seqs ? seqs[i] : (int)i;
-            if ((unsigned)seq < (unsigned)c.max_seqs) {
-                const int len = min((long long)c.lens[seq], (long long)c.max_pages * c.page_tokens);
-                const int pos = positions ? positions[i] : len - 1;
-                if (pos >= 0 && pos < len) {
-                    const int page = c.tables[(size_t)seq * c.max_pages + pos / c.page_tokens];
-                    if ((unsigned)page < (unsigned)c.num_pages) {
-                        ok = true;
-                        at = (((size_t)layer * c.num_pages + page) * c.kv_heads + head) * c.page_tokens +
-                             pos % c.page_tokens;
+    pdl_launch_dependents();
+    const int lane = threadIdx.x & ((1 << lanes_log2) - 1), tok = threadIdx.x >> lanes_log2;
+    const int per_cta = kCopyThreads >> lanes_log2;
+    const long long i = (long long)blockIdx.x * per_cta + tok;
+    const bool in = i < n && lane * 8 < c.head_dim, vals = blockIdx.y & 1;
+    const int h0 = (blockIdx.y >> 1) * heads, count = min(heads, c.kv_heads - h0);
+    const char* from = (const char*)(vals ? v : k) +
+                       (i * stride + (long long)h0 * c.head_dim + lane * 8) * (WIDE ? 4 : 2);
+    const size_t from_step = (size_t)c.head_dim * (WIDE ? 4 : 2);
+    char* to = (char*)(vals ? c.v : c.k);
+    uint8_t* scale = (uint8_t*)(vals ? c.v_scales : c.k_scales);
+    const bool small = c.dtype == AQ_E4M3;
+    const size_t to_step = (size_t)c.page_tokens * c.head_dim * (small ? 1 : 2);
+    bool write = false;
+    for (int h = 0; h < count; h += UNDER_WAY) {
+        Raw<WIDE> x[UNDER_WAY] = {};
+#pragma unroll
+        for (int u = 0; u < UNDER_WAY; ++u) {
+            if (in && h + u < count) x[u].load(from, 0);
+            from += from_step;
+        }
+        if (h == 0) {                              // (the same for the whole CTA)
+            const long long mine = (long long)blockIdx.x * per_cta + threadIdx.x;
+            if (threadIdx.x < per_cta && mine < n) {
+                const int seq = seqs ? seqs[mine] : (int)mine;
+                int p = positions ? positions[mine] : -1;
+                long long slot = -1;
+                if ((unsigned)seq < (unsigned)c.max_seqs) {
+                    const int len = (int)min((long long)c.lens[seq], (long long)c.max_pages * c.page_tokens);
+                    if (!positions) p = len - 1;
+                    if (p >= 0 && p < len) {
+                        const int page = c.tables[(size_t)seq * c.max_pages + p / c.page_tokens];
+                        if ((unsigned)page < (unsigned)c.num_pages)
+                            slot = (((long long)layer * c.num_pages + page) * c.kv_heads + h0) * c.page_tokens +
+                                   p % c.page_tokens;
                     }
                 }
+                if (slot < 0) record_status(status, AQ_ERR_INVALID_ARG);
+                slots[threadIdx.x] = slot;
             }
-            if (!ok && lane == 0) record_status(status, AQ_ERR_INVALID_ARG);
+            __syncthreads();
+            const long long slot = i < n ? slots[tok] : -1;
+            write = in && slot >= 0;
+            to += (slot * c.head_dim + lane * 8) * (small ? 1 : 2);
+            scale += slot;
         }
-        if (in && ok) load8(which ? v : k, (size_t)(i * stride + (long long)head * c.head_dim + lane * 8), x_dt, f);
-        if (c.dtype == AQ_E4M3) {
-            float amax = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
-            for (int d = 1 << lanes_log2 >> 1; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-            const int e = e4m3_scale_exp(amax);
-            if (in && ok) {
-                *(uint2*)((uint8_t*)(which ? c.v : c.k) + at * c.head_dim + lane * 8) = e4m3_pack8(f, pow2f(-e));
-                if (lane == 0) ((uint8_t*)(which ? c.v_scales : c.k_scales))[at] = (uint8_t)(e + 127);
+        for (int u = 0; u < UNDER_WAY; ++u) {
+            const bool now = write && h + u < count;
+            float f[8];
+            x[u].widen(x_dt, f);
+            if (small) {                           // (all lanes take part in the shuffles)
+                float amax = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) {
+                    const float o = __shfl_xor_sync(~0u, amax, d);
+                    if (d < 1 << lanes_log2) amax = fmaxf(amax, o);
+                }
+                const int e = e4m3_scale_exp(amax);
+                if (now) {
+                    *(uint2*)to = e4m3_pack8(f, pow2f(-e));
+                    if (lane == 0) *scale = (uint8_t)(e + 127);
+                }
+                scale += c.page_tokens;
+            } else if (now) {
+                store8(to, 0, c.dtype, f);
             }
-        } else if (in && ok) {
-            store8(which ? c.v : c.k, at * c.head_dim + lane * 8, c.dtype, f);
+            to += to_step;
         }
     }
 }
@@ -403,14 +541,17 @@ aq_status launch_kv_init(const aq_kv_cache& c, cudaStream_t st) {
 
 aq_status launch_kv_reserve(const aq_kv_cache& c, int n, const int* seqs, const int* counts, void* ws,
                             cudaStream_t st) {
-    return launch_dependent(kv_plan_kernel<false>, 1, kPlanThreads, 0, st, c, kv_scratch(c, ws), n, seqs, counts);
+    return launch_dependent(n <= kPlanThreads ? kv_plan_kernel<false> : kv_plan_long_kernel<false>, 1, kPlanThreads, 0, st,
+                            c, kv_scratch(c, ws), n, seqs, counts);
 }
 
 aq_status launch_kv_fork(const aq_kv_cache& c, int n, const int* src, const int* dst, void* ws, cudaStream_t st) {
     const KvScratch s = kv_scratch(c, ws);
     int grid;
     if (aq_status e = copy_grid(c, n, &grid); e != AQ_OK) return e;
-    if (aq_status e = launch_dependent(kv_plan_kernel<true>, 1, kPlanThreads, 0, st, c, s, n, src, dst); e != AQ_OK)
+    if (aq_status e = launch_dependent(n <= kPlanThreads ? kv_plan_kernel<true> : kv_plan_long_kernel<true>, 1,
+                                       kPlanThreads, 0, st, c, s, n, src, dst);
+        e != AQ_OK)
         return e;
     return launch_dependent(kv_share_kernel, grid, kCopyThreads, 0, st, c, s, n, src, dst);
 }
@@ -440,10 +581,17 @@ aq_status launch_kv_write(const aq_kv_cache& c, int layer, int n, const int* seq
     if (aq_status e = device_info(&di); e != AQ_OK) return e;
     int lanes_log2 = 1;
     while ((8 << lanes_log2) < c.head_dim) ++lanes_log2;
-    const size_t per_cta = kCopyThreads >> lanes_log2, rows = (size_t)n * 2 * c.kv_heads;
-    const size_t ctas = (rows + per_cta - 1) / per_cta, most = (size_t)di.sms * 8;
-    return launch_dependent(kv_write_kernel, (unsigned)(ctas < most ? ctas : most), kCopyThreads, 0, st, c, layer, n,
-                            seqs, positions, k, v, x_dt, stride, lanes_log2, (unsigned int*)ws);
+    const long long per_cta = kCopyThreads >> lanes_log2, tokens = (n + per_cta - 1) / per_cta;
+    // A CTA takes as many heads as leaves two CTAs per SM: all of them for prompts (8188 tokens of
+    // 8 heads of 128, bf16 to E4M3: 12.2 us; with eight CTAs per SM 14.3), one for a decode step.
+    long long heads = 2 * c.kv_heads * tokens / (2 * di.sms);
+    heads = heads < 1 ? 1 : heads > c.kv_heads ? c.kv_heads : heads;
+    const dim3 grid((unsigned)tokens, 2 * (unsigned)((c.kv_heads + heads - 1) / heads));
+    const bool wide = x_dt == AQ_F32;
+    return launch_dependent(heads > 1 ? (wide ? kv_write_kernel<4, true> : kv_write_kernel<4, false>)
+                                      : (wide ? kv_write_kernel<1, true> : kv_write_kernel<1, false>), grid,
+                            kCopyThreads, 0, st, c, layer, n, seqs, positions, k, v, x_dt, stride, lanes_log2,
+                            (int)heads, (unsigned int*)ws);
 }
 
 }  // namespace aq

@@ -45,28 +45,6 @@ __device__ __forceinline__ float row_reduce(float v, int row_threads, float* buf
     return v;
 }
 
-// Eight elements as loaded, 16 or 32 bytes, and their widening (dt is the same for all threads).
-template <bool WIDE>
-struct Raw {
-    uint4 v[WIDE ? 2 : 1];
-    __device__ __forceinline__ void load(const void* p, size_t i) {
-        const uint4* q = (const uint4*)((const char*)p + i * (WIDE ? 4 : 2));
-        v[0] = q[0];
-        if constexpr (WIDE) v[1] = q[1];
-    }
-    __device__ __forceinline__ void widen(int dt, float (&f)[8]) const {
-        if constexpr (WIDE) {
-            const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
-        } else if (dt == AQ_F16) {
-            unpack8<AQ_F16>(v[0], f);
-        } else {
-            unpack8<AQ_BF16>(v[0], f);
-        }
-    }
-};
-
 // Eight output values at column c of a row: 16/32-bit, or E4M3 with the block's exponent e.
 __device__ __forceinline__ void put(const NormArgs& a, size_t row, int c, const float (&y)[8], int e) {
     if (a.y_dt == AQ_E4M3) *(uint2*)((uint8_t*)a.y + row * a.cols + c) = e4m3_pack8(y, pow2f(-e));

@@ -143,9 +143,10 @@ class PagedKVCache:
         """Store row i of k and v ([n][kv_heads][head_dim], fp16, bf16 or fp32; rows may be
         strided) as token positions[i] of sequence seqs[i] (default: its last token)."""
         n = self._list(seqs, "seqs")
+        at = None
         if positions is not None:
             self._list(positions, "positions", n)
-            positions = positions.data_ptr()
+            at = positions.data_ptr()
         stride = self._rows(k, "k", n, self.kv_heads)
         code = _FLOATS.get(k.dtype)
         if code is None:
@@ -153,7 +154,7 @@ class PagedKVCache:
         if self._rows(v, "v", n, self.kv_heads) != stride or v.dtype != k.dtype:
             raise ValueError("k and v must have the same dtype and row stride")
         stream, ws, size, _ = self._scratch()
-        status = aq_kv_write(self._ref, layer, n, seqs.data_ptr(), positions, k.data_ptr(), v.data_ptr(),
+        status = aq_kv_write(self._ref, layer, n, seqs.data_ptr(), at, k.data_ptr(), v.data_ptr(),
                              code, stride, ws, size, stream)
         if status:
             raise AQError(status, "aq_kv_write")
@@ -172,9 +173,12 @@ class PagedKVCache:
             raise ValueError("q must be [n][q_heads][head_dim], q_heads a positive multiple of %d" % self.kv_heads)
         n, q_heads = shape[0], shape[1]
         stride = self._rows(q, "q", n, q_heads)
+        # (Arguments keep their names until after the launch: one that only the caller's expression
+        # held would be freed, and its memory given to `out`.)
+        seqs_at = lse_at = None
         if seqs is not None:
             self._list(seqs, "seqs", n)
-            seqs = seqs.data_ptr()
+            seqs_at = seqs.data_ptr()
         if out is None:
             out = torch.empty_like(q) if q.is_contiguous() else torch.empty(shape, dtype=q.dtype, device=self.device)
         elif out.shape != shape or out.dtype != q.dtype or out.get_device() != self._index or \
@@ -184,11 +188,11 @@ class PagedKVCache:
             if lse.shape != shape[:2] or lse.dtype != torch.float32 or \
                     lse.get_device() != self._index or not lse.is_contiguous():
                 raise ValueError("lse must be a contiguous fp32 [n][q_heads] tensor")
-            lse = lse.data_ptr()
+            lse_at = lse.data_ptr()
         stream, ws, size, _ = self._scratch(q_heads)
-        status = aq_kv_attend(self._ref, layer, n, seqs, q.data_ptr(), code, stride, q_heads,
+        status = aq_kv_attend(self._ref, layer, n, seqs_at, q.data_ptr(), code, stride, q_heads,
                               self.head_dim ** -0.5 if scale is None else scale, window,
-                              out.data_ptr(), lse, ws, size, stream)
+                              out.data_ptr(), lse_at, ws, size, stream)
         if status:
             raise AQError(status, "aq_kv_attend")
         return out

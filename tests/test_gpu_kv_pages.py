@@ -296,3 +296,34 @@ def test_binding_refusals():
                  lambda: PagedKVCache.from_tensors(cache.k, cache.v[:, ::2], cache.tables, cache.lens, cache.refs)]:
         with pytest.raises((TypeError, ValueError, RuntimeError)):
             call()
+
+
+def test_lists_of_more_than_a_thousand_sequences():
+    """Entries beyond one CTA's threads: reserve and fork of 1500 sequences, and their refusals."""
+    U.require_gpu()
+    P, page, S, W = 9000, 8, 3200, 6
+    cache = PagedKVCache(P, page, 1, 16, S, W, dtype="f16")
+    model = K.Model(P, page, S, W)
+    scramble(cache, 7)
+    rng = np.random.Generator(np.random.PCG64(8))
+    some = [int(s) for s in rng.permutation(1600)[:1500]]
+    counts = [int(v) for v in rng.integers(0, 30, 1500)]
+
+    def both(op, *lists):
+        before = pools(cache)
+        model.copies = []
+        what = getattr(model, op)(*lists)
+        getattr(cache, op)(*[ints(v) for v in lists])
+        expect(cache, what if op != "free" else "ok")
+        model.assert_same(cache)
+        assert_copied(cache, before, model.copies)
+        return what
+
+    assert both("reserve", some, counts) == "ok"
+    assert both("fork", some, [1600 + i for i in range(1500)]) == "ok"
+    assert both("fork", some, [1600 + i for i in range(1500)]) == "invalid"
+    assert both("reserve", some[:1499] + some[:1]) == "invalid"
+    assert both("reserve", some[:1400], [48] * 1400) == "capacity"
+    assert both("reserve", some) in ("ok", "capacity")
+    assert both("free", some) is None
+    assert both("reserve", list(range(1600, 3100)), [1] * 1500) in ("ok", "capacity")
