@@ -488,20 +488,25 @@ struct Loader {
         const int piece = lane % T::PR, row0 = lane / T::PR;
         const bool real = piece * 16 < a.head_dim * T::ESZ;
         const size_t row_bytes = (size_t)a.head_dim * T::ESZ;
-        const int first = __shfl_sync(~0u, cur, e0 & 31);
-        if (mask >= T::CT - 1 && p.t + T::CT <= p.len && (unsigned)first < (unsigned)a.num_pages) {
-            // all of the chunk is cached, in one page: its rows follow one another
-            const size_t off = (((((size_t)first * a.kv_heads + kvh) << a.page_log2) + (p.t & mask) + row0) * row_bytes) +
-                               (real ? piece * 16 : 0);
-            const uint8_t *k = a.k + off, *v = a.v + off;
+        if (mask >= 15 && p.t + T::CT <= p.len) {
+            // all of the chunk is cached, and 16 rows that follow one another lie in one page
 #pragma unroll
-            for (int r0 = 0; r0 < T::CT; r0 += RPP) {
-                const uint32_t d = stage + swz<T::PR>(r0 + row0, piece);
-                cp16(d, k + r0 * row_bytes, real);
-                cp16(d + T::KV, v + r0 * row_bytes, real);
+            for (int r1 = 0; r1 < T::CT; r1 += 16) {
+                const int page = __shfl_sync(~0u, cur, ((p.t + r1) >> a.page_log2) & 31);
+                const bool ok = (unsigned)page < (unsigned)a.num_pages;
+                if (!ok) record_status(a.status, AQ_ERR_INVALID_ARG);
+                const size_t row = (((size_t)(ok ? page : 0) * a.kv_heads + kvh) << a.page_log2) + ((p.t + r1) & mask) + row0;
+                const size_t off = row * row_bytes + (real ? piece * 16 : 0);
+                const uint8_t *k = a.k + off, *v = a.v + off;
+#pragma unroll
+                for (int r0 = 0; r0 < 16; r0 += RPP) {
+                    const uint32_t d = stage + swz<T::PR>(r1 + r0 + row0, piece);
+                    cp16(d, k + r0 * row_bytes, ok && real);
+                    cp16(d + T::KV, v + r0 * row_bytes, ok && real);
+                }
             }
         } else if (p.t + T::CT <= p.len) {
-            // all cached, in several pages (or a bad one): a pass of at most eight rows has one
+            // pages of eight tokens: a pass of at most eight rows has one
 #pragma unroll
             for (int r0 = 0; r0 < T::CT; r0 += RPP) {
                 const int page = __shfl_sync(~0u, cur, ((p.t + r0) >> a.page_log2) & 31);
