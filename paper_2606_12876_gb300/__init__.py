@@ -370,47 +370,19 @@ def aq_kv_init(cache, stream=None):
     _check(lib().aq_kv_init(ctypes.byref(cache), _stream(stream)), "aq_kv_init")
 
 
-def aq_kv_reserve(cache, n, seqs, counts, workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_reserve(ctypes.byref(cache), n, _ptr(seqs), _ptr(counts), _ptr(workspace),
-                               workspace_bytes, _stream(stream)), "aq_kv_reserve")
+# The calls of a decode step. They take a cache as ctypes.byref(KVCache), addresses and the raw
+# stream as integers, in the order of aq.h, and return the status: their callers (kv.py, norm.py)
+# have these at hand, and on small batches the host's time per call is what counts.
+def _direct(name):
+    def call(*args):
+        return getattr(_lib or lib(), name)(*args)
+    call.__name__, call.__doc__ = name, "%s of aq.h, arguments as there; returns the status." % name
+    return call
 
 
-def aq_kv_fork(cache, n, src, dst, workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_fork(ctypes.byref(cache), n, _ptr(src), _ptr(dst), _ptr(workspace),
-                            workspace_bytes, _stream(stream)), "aq_kv_fork")
-
-
-def aq_kv_free(cache, n, seqs, workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_free(ctypes.byref(cache), n, _ptr(seqs), _ptr(workspace), workspace_bytes,
-                            _stream(stream)), "aq_kv_free")
-
-
-def aq_kv_compact(cache, used, workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_compact(ctypes.byref(cache), _ptr(used), _ptr(workspace), workspace_bytes,
-                               _stream(stream)), "aq_kv_compact")
-
-
-def aq_kv_copy_pages(cache, n, src, dst, workspace, workspace_bytes, stream=None):
-    _check(lib().aq_kv_copy_pages(ctypes.byref(cache), n, _ptr(src), _ptr(dst), _ptr(workspace),
-                                  workspace_bytes, _stream(stream)), "aq_kv_copy_pages")
-
-
-# The three calls of a decode step's inner loop take addresses and the raw stream as integers and
-# return the status: their callers (kv.py, norm.py) have them at hand, and on small batches the
-# host's time per call is what counts.
-def aq_kv_write(*args):
-    """aq_kv_write of aq.h; a cache is passed as ctypes.byref(KVCache). Returns the status."""
-    return (_lib or lib()).aq_kv_write(*args)
-
-
-def aq_kv_attend(*args):
-    """aq_kv_attend of aq.h; a cache is passed as ctypes.byref(KVCache). Returns the status."""
-    return (_lib or lib()).aq_kv_attend(*args)
-
-
-def aq_rmsnorm(*args):
-    """aq_rmsnorm of aq.h. Returns the status."""
-    return (_lib or lib()).aq_rmsnorm(*args)
+aq_kv_reserve, aq_kv_fork, aq_kv_free, aq_kv_compact, aq_kv_copy_pages, aq_kv_write, aq_kv_attend, \
+    aq_rmsnorm = [_direct(n) for n in ("aq_kv_reserve", "aq_kv_fork", "aq_kv_free", "aq_kv_compact",
+                                       "aq_kv_copy_pages", "aq_kv_write", "aq_kv_attend", "aq_rmsnorm")]
 
 
 def aq_selftest_read(src, nbytes, sink, stream=None):

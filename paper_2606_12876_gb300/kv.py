@@ -98,7 +98,9 @@ class PagedKVCache:
 
     def _pages(self, call, *args):
         stream, ws, size, _ = self._scratch()
-        call(self._c, *args, ws, size, stream)
+        status = call(self._ref, *args, ws, size, stream)
+        if status:
+            raise AQError(status, call.__name__)
 
     def _list(self, t, what, n=None):
         if t.dtype != _INT32 or t.get_device() != self._index or t.dim() != 1 or not t.is_contiguous():
@@ -113,31 +115,31 @@ class PagedKVCache:
         n = self._list(seqs, "seqs")
         if counts is not None:
             self._list(counts, "counts", n)
-        self._pages(aq_kv_reserve, n, seqs, counts)
+        self._pages(aq_kv_reserve, n, seqs.data_ptr(), None if counts is None else counts.data_ptr())
 
     def fork(self, src, dst):
         """Make the empty sequences dst copies of src: full pages are shared, a partial last page
         is copied; all or nothing (see check)."""
         n = self._list(src, "src")
         self._list(dst, "dst", n)
-        self._pages(aq_kv_fork, n, src, dst)
+        self._pages(aq_kv_fork, n, src.data_ptr(), dst.data_ptr())
 
     def free(self, seqs):
         """Release the listed sequences and the pages that no other sequence holds."""
-        self._pages(aq_kv_free, self._list(seqs, "seqs"), seqs)
+        self._pages(aq_kv_free, self._list(seqs, "seqs"), seqs.data_ptr())
 
     def compact(self, used=None):
         """Move the pages in use to the lowest indices; used: an int32 tensor of one element that
         receives their number, or None."""
         if used is not None:
             self._list(used, "used", 1)
-        self._pages(aq_kv_compact, used)
+        self._pages(aq_kv_compact, None if used is None else used.data_ptr())
 
     def copy_pages(self, src, dst):
         """Copy pages src to pages dst in all layers (dst distinct, none of them in src)."""
         n = self._list(src, "src")
         self._list(dst, "dst", n)
-        self._pages(aq_kv_copy_pages, n, src, dst)
+        self._pages(aq_kv_copy_pages, n, src.data_ptr(), dst.data_ptr())
 
     def write(self, k, v, seqs, positions=None, layer=0):
         """Store row i of k and v ([n][kv_heads][head_dim], fp16, bf16 or fp32; rows may be

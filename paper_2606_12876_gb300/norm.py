@@ -6,16 +6,10 @@ from . import AQ_BF16, AQ_E4M3, AQ_F16, AQ_F32, AQError, aq_rmsnorm, _stream_of
 _CODES = {torch.float16: AQ_F16, torch.bfloat16: AQ_BF16, torch.float32: AQ_F32}
 
 
-def _code(t):
-    code = _CODES.get(t.dtype)
-    if code is None:
-        raise TypeError("unsupported dtype %s" % t.dtype)
-    return code
-
-
 def _norm(x, weight, eps, residual, residual_out, y, y_code, scales, block):
     # The checks and the call; returns the tensor that received h, or None.
-    rows, cols = x.shape
+    shape = x.shape
+    rows, cols = shape
     x_stride, one = x.stride()
     index = x.get_device()
     if (one != 1 and cols > 1) or index < 0:
@@ -23,22 +17,28 @@ def _norm(x, weight, eps, residual, residual_out, y, y_code, scales, block):
     if weight.shape != (cols,) or not weight.is_contiguous() or weight.get_device() != index:
         raise ValueError("weight must be a contiguous [%d] tensor on x's device" % cols)
     r, r_out, r_code = None, None, AQ_F32
-    if residual is not None:
-        if residual.shape != x.shape or not residual.is_contiguous() or residual.get_device() != index:
-            raise ValueError("the residual must be contiguous, of x's shape and on its device")
-        if residual_out is None:
-            residual_out = torch.empty_like(residual)
-        elif residual_out.dtype != residual.dtype:
-            raise ValueError("residual_out must have the residual's dtype")
-        r = residual.data_ptr()
-    if residual_out is not None:
-        if residual_out.shape != x.shape or not residual_out.is_contiguous() or \
-                residual_out.get_device() != index:
-            raise ValueError("residual_out must be contiguous, of x's shape and on its device")
-        r_code, r_out = _code(residual_out), residual_out.data_ptr()
-    status = aq_rmsnorm(rows, cols, x.data_ptr(), _code(x), x_stride if rows > 1 else cols, r, r_out, r_code,
-                        weight.data_ptr(), _code(weight), eps, y.data_ptr(), y_code, scales, block,
-                        _stream_of(index))
+    try:
+        x_code, w_code = _CODES[x.dtype], _CODES[weight.dtype]
+        if residual is not None:
+            if residual.shape != shape or not residual.is_contiguous() or residual.get_device() != index:
+                raise ValueError("the residual must be contiguous, of x's shape and on its device")
+            r, r_code = residual.data_ptr(), _CODES[residual.dtype]
+            if residual_out is None:
+                residual_out = torch.empty_like(residual)
+                r_out = residual_out.data_ptr()
+        if residual_out is not None and r_out is None:
+            if residual_out.shape != shape or not residual_out.is_contiguous() or \
+                    residual_out.get_device() != index:
+                raise ValueError("residual_out must be contiguous, of x's shape and on its device")
+            r_out = residual_out.data_ptr()
+            if residual is None:
+                r_code = _CODES[residual_out.dtype]
+            elif residual_out.dtype != residual.dtype:
+                raise ValueError("residual_out must have the residual's dtype")
+    except KeyError as e:
+        raise TypeError("unsupported dtype %s" % e.args[0]) from None
+    status = aq_rmsnorm(rows, cols, x.data_ptr(), x_code, x_stride if rows > 1 else cols, r, r_out, r_code,
+                        weight.data_ptr(), w_code, eps, y.data_ptr(), y_code, scales, block, _stream_of(index))
     if status:
         raise AQError(status, "aq_rmsnorm")
     return residual_out
@@ -55,7 +55,10 @@ def rmsnorm(x, weight, eps=1e-5, residual=None, residual_out=None, y_dtype=None,
             y = torch.empty(x.shape, dtype=x.dtype if y_dtype is None else y_dtype, device=x.device)
     elif y.shape != x.shape or not y.is_contiguous() or y.get_device() != x.get_device():
         raise ValueError("y must be contiguous, of x's shape and on its device")
-    return y, _norm(x, weight, eps, residual, residual_out, y, _code(y), None, 0)
+    code = _CODES.get(y.dtype)
+    if code is None:
+        raise TypeError("unsupported output dtype %s" % y.dtype)
+    return y, _norm(x, weight, eps, residual, residual_out, y, code, None, 0)
 
 
 def rmsnorm_8bit(x, weight, eps=1e-5, residual=None, residual_out=None, block=32):
