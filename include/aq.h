@@ -513,7 +513,7 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  *   workspace: aq_kv_attend_workspace_bytes(cache, n, q_heads) bytes, 16-byte aligned,
  *              zero-filled before first use; calls that may overlap must not share one.
  * seqs may name a sequence several times; NULL needs n <= max_seqs. One kernel per 512 entries:
- * the cache is read once, in equal shares of 16- or 32-token chunks whatever the lengths are, and
+ * the cache is read once, in equal shares of chunks of 16 to 64 tokens whatever the lengths are, and
  * the shares' results are joined in the order of the tokens, so the result does not depend on
  * scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
  * the longest possible length, and AQ_ERR_INVALID_ARG recorded.

@@ -50,10 +50,10 @@ struct Tile {
     static constexpr int ESZ = DT == AQ_E4M3 ? 1 : 2;
     static constexpr int RB = HD * ESZ;                      // bytes of a token's row
     static constexpr int PR = RB / 16;                       // 16-byte pieces of a row
-    static constexpr int CT = (HD == 64 || (HD == 128 && ESZ == 1)) ? 32 : 16;   // tokens per chunk
+    static constexpr int CT = RB == 64 ? 64 : RB == 128 ? 32 : 16;   // tokens per chunk
     static constexpr int KV = CT * RB;                       // bytes of a chunk's keys (or values)
     static constexpr int STAGE = 2 * KV + (ESZ == 1 ? 128 : 0);   // keys, values, scale bytes
-    static constexpr int NS = STAGE <= 4224 ? 6 : HD == 256 && ESZ == 1 ? 5 : 3;
+    static constexpr int NS = HD == 256 && ESZ == 1 ? 5 : 3;
     static constexpr int RING = NS * STAGE;                  // a warp's ring
     static constexpr int ROWS = 8 * NH;                      // query heads of a tile
     static constexpr int OS = HD + 4;                        // floats from one row of a partial's o to the next
@@ -536,12 +536,12 @@ struct Loader {
         }
         if constexpr (DT == AQ_E4M3) {
             // scale bytes, four tokens (of one page) a lane: keys' at 2 KV, values' at 2 KV + 64
-            const int r = (lane & 7) * 4, tok = p.t + r;
+            const int r = (lane & 15) * 4, tok = p.t + r;
             const int page = __shfl_sync(~0u, cur, (tok >> a.page_log2) & 31);
             const bool ok = tok < p.len && (unsigned)page < (unsigned)a.num_pages;
             const size_t at = ok ? (((size_t)page * a.kv_heads + kvh) << a.page_log2) + (tok & mask) : 0;
-            if (lane < 16 && r < T::CT) {
-                const bool vals = lane >= 8;
+            if (r < T::CT) {
+                const bool vals = lane >= 16;
                 cp4(stage + 2 * T::KV + (vals ? 64 : 0) + r, (vals ? a.vs : a.ks) + at, ok);
             }
         }
