@@ -53,15 +53,18 @@ struct Tile {
     static constexpr int CT = RB == 64 ? 64 : RB == 128 ? 32 : 16;   // tokens per chunk
     static constexpr int KV = CT * RB;                       // bytes of a chunk's keys (or values)
     static constexpr int STAGE = 2 * KV + (ESZ == 1 ? 128 : 0);   // keys, values, scale bytes
-    static constexpr int NS = HD == 256 && ESZ == 1 ? 5 : 3;
-    static constexpr int RING = NS * STAGE;                  // a warp's ring
+    // Two stages a warp, 128 KB a CTA: with three the SMs' queues grow and some get their data
+    // later than others (a 3.5 GB cache 530 us, with two 511).
+    static constexpr int NS = 2;
     static constexpr int ROWS = 8 * NH;                      // query heads of a tile
     static constexpr int OS = HD + 4;                        // floats from one row of a partial's o to the next
     static constexpr int PART = 2 * ROWS + ROWS * OS;        // floats of a partial: maxima, sums, o
-    static_assert(RING >= 2 * PART * 4 && PART % 4 == 0, "a warp's ring holds its two pieces at the end");
-    static constexpr int WARPS = HD == 256 ? 4 : 8;
+    // a warp's ring, which takes its last piece in the end, then a place for its first piece
+    static constexpr int RING = NS * STAGE > PART * 4 ? NS * STAGE : PART * 4;
+    static constexpr int PER_WARP = (RING + PART * 4 + 127) / 128 * 128;
+    static constexpr int WARPS_LOG2 = 8 * PER_WARP <= 210 * 1024 ? 3 : 2, WARPS = 1 << WARPS_LOG2;
     static constexpr int THREADS = 32 * WARPS;
-    static constexpr int SMEM = WARPS * RING;
+    static constexpr int SMEM = WARPS * PER_WARP;
 };
 constexpr int SEG = 2;                                       // chunks that a segment's start and end count for
 
@@ -74,7 +77,6 @@ struct Args {
     unsigned int* status;
     int* arrived;                     // CTAs that have left their partial, by segment or group; 0 between calls
     float* part;                      // [CTA][2][PART]: partials of segments that cross CTAs
-    float* first;                     // [CTA * warps][PART]: first pieces of the warps' shares
     long long q_stride;
     float scale;
     int n, q_heads, kv_heads, group, tiles_per_head, head_dim, page_log2, num_pages, max_seqs, max_pages, window, q_dt;
@@ -805,7 +807,7 @@ __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::W
             if (pass == 0 && threadIdx.x == y0) s.cross[w] = {j0, ctas, rows, q_row};
             if (r >= seg_rows) continue;
             if (of_seg >> lane & 1)
-                list[__popc(of_seg & ((1u << lane) - 1))] = (const float*)(ring + (lane >> 1) * T::RING) + (lane & 1) * T::PART;
+                list[__popc(of_seg & ((1u << lane) - 1))] = (const float*)(ring + (lane >> 1) * T::PER_WARP) + (lane & 1 ? 0 : T::RING / 4);
             __syncwarp();
             float* const dst = pass == 1 ? nullptr : a.part + ((size_t)blockIdx.x * 2 + w) * T::PART;
             for (; r < seg_rows; r += kWarps)
@@ -892,14 +894,13 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
     const long long u0 = min(total, cta0 + share * warp), u1 = min(total, u0 + share);
     if (cta0 >= cta1) return;
 
-    float* const first = a.first + (size_t)(blockIdx.x * kWarps) * T::PART;    // first pieces: global
     if (lane < 2) piece_seg[2 * warp + lane] = -1;
     if (threadIdx.x < 2) s.cross[threadIdx.x].count = 0;
     __syncwarp();
     Place at;
     if (u0 < u1) place_at<T::CT>(a, base, range, seq_of, u0, at);
     if (u0 < u1 && at.pos < u1) {
-        const uint32_t stages = smem_u32(ring + warp * T::RING);
+        const uint32_t stages = smem_u32(ring + warp * T::PER_WARP);
         Place in = at;
         bool more = true;                          // chunk `in` is still to be issued
         Loader<DT, HD> loader;
@@ -943,8 +944,8 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
                 write_final<DT, HD, NH>(a, at, acc, lane);
             } else {
                 // The ring is free once the share's last chunk has been read (only empty groups
-                // of copies are left then); an earlier piece waits in global memory.
-                float* dst = last ? (float*)(ring + warp * T::RING) + T::PART : first + warp * T::PART;
+                // of copies are left then); an earlier piece has a place of its own.
+                float* dst = (float*)(ring + warp * T::PER_WARP) + (last ? 0 : T::RING / 4);
                 write_partial<DT, HD, NH>(a, at.tile, acc, dst, lane);
                 if (lane == 0) piece_seg[2 * warp + last] = at.i * tiles + at.tile;
             }
@@ -955,14 +956,6 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
             acc.clear();
         }
     }
-    __syncwarp();
-    if (piece_seg[2 * warp] >= 0) {                // the first piece, to where the ring was
-        const float* src = first + warp * T::PART;
-        const uint32_t dst = smem_u32(ring + warp * T::RING);
-        for (int x = lane; x < T::PART / 4; x += 32) cp16(dst + x * 16, src + x * 4, true);
-        cp_async_commit();
-        cp_async_wait<0>();
-    }
     __syncthreads();
     finish<DT, HD, NH>(a, s, ring, share, cta0, cta1);
 }
@@ -970,7 +963,7 @@ __global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(
 template <int DT, int HD, int NH>
 size_t attend_ws() {
     using T = Tile<DT, HD, NH>;
-    return kWsStatusBytes + kArrivedBytes + (size_t)kMaxCtas * (2 + T::WARPS) * T::PART * 4;
+    return kWsStatusBytes + kArrivedBytes + (size_t)kMaxCtas * 2 * T::PART * 4;
 }
 
 template <int DT, int HD, int NH>
@@ -990,7 +983,6 @@ aq_status attend(Args a, const DeviceInfo& di, int n, cudaStream_t st) {
     char* ws = (char*)a.status;
     a.arrived = (int*)(ws + kWsStatusBytes);
     a.part = (float*)(ws + kWsStatusBytes + kArrivedBytes);
-    a.first = a.part + (size_t)ctas * 2 * T::PART;
     a.tiles_per_head = (a.group + T::ROWS - 1) / T::ROWS;
     for (int i0 = 0; i0 < n; i0 += kSliceSeqs) {
         Args s = a;
