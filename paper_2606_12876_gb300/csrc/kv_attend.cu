@@ -867,7 +867,7 @@ __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::W
 }
 
 template <int DT, int HD, int NH>
-__global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS)) kv_attend_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__((Tile<DT, HD, NH>::THREADS), 1) kv_attend_kernel(const __grid_constant__ Args a) {
     using T = Tile<DT, HD, NH>;
     constexpr int kWarps = T::WARPS, kThreads = T::THREADS;
     extern __shared__ __align__(1024) uint8_t ring[];
