@@ -427,7 +427,8 @@ typedef struct aq_kv_cache {
     int32_t kv_heads;       /* 1..16384 */
     int32_t head_dim;       /* a multiple of 16, 16..256 */
     int32_t max_seqs;       /* sequence slots, >= 1 */
-    int32_t max_pages;      /* entries of a sequence's table, >= 1 (max_pages * page_tokens < 2^31) */
+    int32_t max_pages;      /* entries of a sequence's table, >= 1; max_pages * page_tokens
+                               <= 2^31 - 1024 */
     int32_t dtype;          /* AQ_F16, AQ_BF16 or AQ_E4M3 */
     void* k;                /* device, [layers][num_pages][kv_heads][page_tokens][head_dim] of dtype */
     void* v;                /* as k */
@@ -501,17 +502,18 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  *     s_t = scale * q . k_t,  out = sum_t p_t v_t / sum_t p_t,  p_t = exp(s_t - max s),
  *     lse = ln sum_t exp(s_t),       over t = max(0, L - window) .. L-1, L = lens[seqs[i]]
  * Query head h reads kv head h / (q_heads / kv_heads). A sequence of length 0 gives zeros and
- * lse = -inf. Cached tokens that are not seen (past the length, before the window) are not read.
+ * lse = -inf (so does one whose scores are all -inf). Cached tokens that are not seen (past the length, before the window) are not read.
  *   q        : device, n rows of [q_heads][head_dim] of q_dtype, 16-byte aligned, q_stride
  *              elements apart (>= q_heads * head_dim, a multiple of 8); q_dtype is the cache's
  *              type, or AQ_F16 / AQ_BF16 for an AQ_E4M3 cache
- *   q_heads  : a positive multiple of kv_heads
+ *   q_heads  : a positive multiple of kv_heads, at most 2^20
  *   scale    : a finite number (usually head_dim^-0.5)
  *   window   : tokens seen from the end, or 0 for all
  *   out      : device, [n][q_heads][head_dim] of q_dtype
  *   lse      : device, [n][q_heads] floats (4-byte aligned), or NULL
  *   workspace: aq_kv_attend_workspace_bytes(cache, n, q_heads) bytes, 16-byte aligned,
- *              zero-filled before first use; calls that may overlap must not share one.
+ *              zero-filled before first use and used by aq_kv_attend alone (it holds counters that
+ *              every call leaves at zero); calls that may overlap must not share one.
  * seqs may name a sequence several times; NULL needs n <= max_seqs. One kernel per 512 entries:
  * the cache is read once, in equal shares of chunks of 16 to 64 tokens whatever the lengths are, and
  * the shares' results are joined in the order of the tokens, so the result does not depend on

@@ -1,7 +1,8 @@
 // C entry points of the key-value cache and the RMS norm (include/aq.h): argument validation and
 // dispatch to the launchers.
-#include <cmath>
 #include <climits>
+#include <cmath>
+#include <initializer_list>
 
 #include "kv.cuh"
 
@@ -18,7 +19,8 @@ aq_status check_cache(const aq_kv_cache* c) {
     if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)))
         return AQ_ERR_UNSUPPORTED;
     if (c->head_dim % 16 || c->head_dim > 256) return AQ_ERR_UNSUPPORTED;
-    if ((long long)c->max_pages * c->page_tokens > INT_MAX || c->kv_heads > 16384) return AQ_ERR_UNSUPPORTED;
+    // (token numbers are ints, with room for a chunk past the last one)
+    if ((long long)c->max_pages * c->page_tokens > INT_MAX - 1023 || c->kv_heads > 16384) return AQ_ERR_UNSUPPORTED;
     return AQ_OK;
 }
 
@@ -153,7 +155,7 @@ aq_status aq_kv_attend(const aq_kv_cache* cache, int layer, int n, const int32_t
         !std::isfinite(scale))
         return AQ_ERR_INVALID_ARG;
     if (q_dtype != AQ_F16 && q_dtype != AQ_BF16) return AQ_ERR_INVALID_ARG;
-    if (cache->dtype != AQ_E4M3 && q_dtype != cache->dtype) return AQ_ERR_UNSUPPORTED;
+    if ((cache->dtype != AQ_E4M3 && q_dtype != cache->dtype) || q_heads > 1 << 20) return AQ_ERR_UNSUPPORTED;
     if (q_stride < (int64_t)q_heads * cache->head_dim) return AQ_ERR_INVALID_ARG;
     if (!seqs && n > cache->max_seqs) return AQ_ERR_INVALID_ARG;
     if (n == 0) return AQ_OK;

@@ -91,6 +91,8 @@ class PagedKVCache:
         stream = _stream_of(self._index)
         got = self._ws.get((stream, q_heads))
         if got is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the first call on a stream allocates a workspace: make one before capturing")
             n = kv_attend_workspace_bytes(self._c, 1, q_heads) if q_heads else kv_workspace_bytes(self._c)
             ws = workspace(n, self.device)
             got = self._ws[(stream, q_heads)] = (stream, ws.data_ptr(), ws.numel(), ws)

@@ -62,10 +62,19 @@ CASES = [  # lengths, q heads, kv heads, head dim, page, type, window
     ([5000], 8, 8, 128, 64, "f16", 4097),
     ([70000, 9], 4, 1, 64, 16, "f16", 0),
     ([40000], 16, 2, 128, 32, "e4m3", 0),
+    # tiles of 9 to 16 query heads at the largest head dimensions
+    ([300, 0, 77, 2000], 32, 2, 256, 32, "bf16", 0),
+    ([300, 0, 77, 2000], 24, 2, 208, 16, "e4m3", 50),
+    ([300, 1, 77, 9000], 12, 1, 128, 64, "e4m3", 0),
+    ([9000], 16, 1, 256, 64, "f16", 0),
+    # many short segments per warp, and equal ones of about a warp's share
+    ([17] * 300, 8, 4, 64, 16, "bf16", 0),
+    ([1000] * 130, 32, 8, 128, 16, "bf16", 0),
+    ([1000] * 130, 8, 8, 128, 16, "e4m3", 0),
 ]
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "%s-%dx%dx%d-p%d-%s-w%d" % (("_".join(map(str, c[0])),) + c[1:]))
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "%s-%dx%dx%d-p%d-%s-w%d" % (("_".join(map(str, c[0][:9])) + "n%d" % len(c[0]),) + c[1:]))
 def test_attend(case):
     U.require_gpu()
     lens, qh, kh, hd, page, dt, window = case
@@ -199,3 +208,18 @@ def test_refusals():
         with pytest.raises((TypeError, ValueError, RuntimeError)):
             cache.attend(**kw)
     assert cache.attend(q[:0]).shape == (0, 4, 64)
+
+
+def test_first_call_inside_a_capture_is_refused():
+    U.require_gpu()
+    cache = K.filled_cache(PagedKVCache, [50, 20], 16, 2, 64, "f16", seed=14)
+    q = query(2, 4, 64, torch.float16)
+    out, graph, x = torch.empty_like(q), torch.cuda.CUDAGraph(), torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        with pytest.raises(RuntimeError):
+            cache.attend(q, out=out)
+    torch.cuda.synchronize()
+    cache.attend(q, out=out)
+    cache.check()

@@ -28,7 +28,8 @@ BAD_CACHES = [(dict(layers=0), INV), (dict(num_pages=0), INV), (dict(kv_heads=0)
               (dict(max_pages=-1), INV), (dict(head_dim=0), INV), (dict(page_tokens=0), INV), (dict(dtype=2), INV),
               (dict(dtype=4), INV), (dict(page_tokens=4), UNS), (dict(page_tokens=24), UNS),
               (dict(page_tokens=2048), UNS), (dict(head_dim=72), UNS), (dict(head_dim=272), UNS),
-              (dict(max_pages=1 << 28, page_tokens=16), UNS)]
+              (dict(max_pages=1 << 28, page_tokens=16), UNS), (dict(max_pages=(1 << 27) - 1, page_tokens=16), UNS),
+              (dict(kv_heads=16385), UNS)]
 BAD_BOOKS = [(dict(tables=None), INV), (dict(lens=None), INV), (dict(refs=None), INV), (dict(lens=FAKE + 2), ALI)]
 BAD_POOLS = [(dict(k=None), INV), (dict(v=None), INV), (dict(k=FAKE + 8), ALI),
              (dict(dtype=aq.AQ_E4M3), INV), (dict(dtype=aq.AQ_E4M3, k_scales=FAKE, v_scales=FAKE + 8), ALI)]
@@ -106,7 +107,7 @@ def test_attend_arguments():
                               BIG, None)
 
     for kw, status in [(dict(layer=2), INV), (dict(layer=-1), INV), (dict(heads=0), INV), (dict(heads=3), INV),
-                       (dict(qd=aq.AQ_F32), INV), (dict(qd=aq.AQ_F16), UNS), (dict(stride=248), INV),
+                       (dict(qd=aq.AQ_F32), INV), (dict(heads=(1 << 20) + 2, stride=1 << 30), UNS), (dict(qd=aq.AQ_F16), UNS), (dict(stride=248), INV),
                        (dict(stride=260), ALI), (dict(q=None), INV), (dict(out=None), INV), (dict(q=FAKE + 8), ALI),
                        (dict(out=FAKE + 4), ALI), (dict(lse=FAKE + 2), ALI), (dict(window=-1), INV),
                        (dict(scale=float("inf")), INV), (dict(scale=float("nan")), INV)]:
