@@ -24,7 +24,7 @@
 //
 // Measured on a GB300 (copy peak 6.79 TB/s): 48 sequences of 8192 to 32768 tokens, 8 heads of 128,
 // bf16 (3.5 GB): 506 us; one sequence of 131071 tokens, fp16: 85.9 us (6.25 TB/s); 64 sequences of
-// 17 to 2048 tokens: 29.3 us; 64 query heads over an E4M3 cache of 380 MB: 70.5 us (5.4 TB/s). What a
+// 17 to 2048 tokens: 28.8 us; 64 query heads over an E4M3 cache of 380 MB: 69.9 us (5.4 TB/s). What a
 // call costs beside its bytes, about 4 us until the first keys arrive (lengths, table, keys: three
 // dependent reads) and 5 to 8 us to merge and join, is latency.
 //
@@ -72,7 +72,9 @@ struct Tile {
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int SMEM = WARPS * PER_WARP;
 };
-constexpr int SEG = 2;                                       // chunks that a segment's start and end count for
+// Chunks that a segment's start and end count for in the shares (64 ragged sequences: 31.5 us with 1,
+// 28.8 with 3, 28.8 with 6; many equal short ones lose a little with more).
+constexpr int SEG = 3;
 
 struct Args {
     const uint8_t *k, *v, *ks, *vs;   // the layer's pools
