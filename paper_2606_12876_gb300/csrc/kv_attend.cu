@@ -467,7 +467,8 @@ __device__ __forceinline__ void load_query(const Args& a, const Place& p, int la
 }
 
 // Issues the copies of one chunk into a stage: the warp's lanes take 16-byte pieces, each of its
-// token's page. cur/nxt hold 32 table entries each, one a lane, from entry 32 * block on.
+// token's page; tokens that are not seen become zeros (a weight of 0 times what happens to be
+// there would not do). cur/nxt hold 32 table entries each, one a lane, from entry 32 * block on.
 template <int DT, int HD>
 struct Loader {
     using T = Tile<DT, HD, 1>;
@@ -498,8 +499,9 @@ struct Loader {
         const int piece = lane % T::PR, row0 = lane / T::PR;
         const bool real = piece * 16 < a.head_dim * T::ESZ;
         const size_t row_bytes = (size_t)a.head_dim * T::ESZ;
-        if (mask >= 15 && p.t + T::CT <= p.len) {
-            // all of the chunk is cached, and 16 rows that follow one another lie in one page
+        const bool full = p.t >= p.lo && p.t + T::CT <= p.len;
+        if (mask >= 15 && full) {
+            // all of the chunk is seen, and 16 rows that follow one another lie in one page
 #pragma unroll
             for (int r1 = 0; r1 < T::CT; r1 += 16) {
                 const int page = __shfl_sync(~0u, cur, ((p.t + r1) >> a.page_log2) & 31);
@@ -515,7 +517,7 @@ struct Loader {
                     cp16(d + T::KV, v + r0 * row_bytes, ok && real);
                 }
             }
-        } else if (p.t + T::CT <= p.len) {
+        } else if (full) {
             // pages of eight tokens: a pass of at most eight rows has one
 #pragma unroll
             for (int r0 = 0; r0 < T::CT; r0 += RPP) {
@@ -535,7 +537,7 @@ struct Loader {
             for (int r = row0; r < T::CT; r += RPP) {
                 const int tok = p.t + r;
                 const int page = __shfl_sync(~0u, cur, (tok >> a.page_log2) & 31);
-                const bool in = tok < p.len, ok = in && (unsigned)page < (unsigned)a.num_pages;
+                const bool in = tok >= p.lo && tok < p.len, ok = in && (unsigned)page < (unsigned)a.num_pages;
                 if (in && !ok) record_status(a.status, AQ_ERR_INVALID_ARG);
                 const size_t at = ok ? (((size_t)page * a.kv_heads + kvh) << a.page_log2) + (tok & mask) : 0;
                 const size_t off = ok && real ? at * row_bytes + piece * 16 : 0;
@@ -548,6 +550,7 @@ struct Loader {
             // scale bytes, four tokens (of one page) a lane: keys' at 2 KV, values' at 2 KV + 64
             const int r = (lane & 15) * 4, tok = p.t + r;
             const int page = __shfl_sync(~0u, cur, (tok >> a.page_log2) & 31);
+            // (four tokens at a time, unseen ones among them: their scores are masked)
             const bool ok = tok < p.len && (unsigned)page < (unsigned)a.num_pages;
             const size_t at = ok ? (((size_t)page * a.kv_heads + kvh) << a.page_log2) + (tok & mask) : 0;
             if (r < T::CT) {
@@ -609,6 +612,8 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
     for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+            const int tok = p.t + tt * 16 + h * 8 + row;
+            const bool out = edge && (tok < p.lo || tok >= p.len);
             float kf = 1.0f;
             if constexpr (DT == AQ_E4M3) {
                 uint32_t kb, vb;
@@ -617,10 +622,8 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vb) : "r"(at + 64) : "memory");
                 kf = __uint_as_float(kb << 23);
                 vexp[tt][h] = (float)((int)vb - 127);
-                vfac[tt][h] = __uint_as_float(vb << 23);
+                vfac[tt][h] = out ? 0.0f : __uint_as_float(vb << 23);   // (an unseen token's byte may be anything)
             }
-            const int tok = p.t + tt * 16 + h * 8 + row;
-            const bool out = edge && (tok < p.lo || tok >= p.len);
 #pragma unroll
             for (int g = 0; g < NH; ++g)
 #pragma unroll

@@ -136,6 +136,41 @@ def test_offsets_past_32_bits():
     check(cache, query(2, 16, 128, torch.bfloat16))
 
 
+@pytest.mark.parametrize("dt,page,window", [("f16", 16, 33), ("bf16", 8, 5), ("e4m3", 32, 70), ("e4m3", 8, 1)])
+def test_nan_before_the_window_is_not_seen(dt, page, window):
+    """Tokens that the window leaves out hold NaN (8-bit ones with a NaN code and the largest
+    scale): also those that share a chunk with tokens that are seen."""
+    U.require_gpu()
+    lens = [100, 37, 3, 250]
+    cache = K.filled_cache(PagedKVCache, lens, page, 2, 64, dt, seed=16)
+    for s, n in enumerate(lens):
+        for t in range(max(0, n - window)):
+            at = int(cache.tables[s, t // page])
+            for pool, scales in ((cache.k, cache.k_scales), (cache.v, cache.v_scales)):
+                if scales is None:
+                    pool[0, at, :, t % page] = float("nan")
+                else:
+                    pool.view(torch.uint8)[0, at, :, t % page] = 0x7f
+                    scales[0, at, :, t % page] = 254
+    check(cache, query(4, 8, 64, DT.get(dt, torch.float16)), window=window)
+
+
+def test_scale_bytes_of_unseen_slots_do_not_matter():
+    """The extreme scale bytes in slots past a length, which are fetched four at a time with seen ones."""
+    U.require_gpu()
+    lens = [5, 33, 62, 1, 127]
+    cache = K.filled_cache(PagedKVCache, lens, 16, 2, 64, "e4m3", seed=17)
+    q = query(5, 8, 64, torch.bfloat16)
+    want = check(cache, q)
+    for byte in (0, 1, 127, 254, 255):
+        for s, n in enumerate(lens):
+            for t in range(n, -(-n // 16) * 16):
+                at = int(cache.tables[s, t // 16])
+                cache.k_scales[0, at, :, t % 16] = byte
+                cache.v_scales[0, at, :, t % 16] = byte
+        assert torch.equal(cache.attend(q), want), byte
+
+
 def test_nan_in_a_cached_value_reaches_its_rows_only():
     U.require_gpu()
     cache = K.filled_cache(PagedKVCache, [50, 60], 16, 2, 64, "f16", seed=10)
