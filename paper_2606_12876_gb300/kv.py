@@ -82,8 +82,8 @@ class PagedKVCache:
         self._q_codes = {torch.float16: AQ_F16, torch.bfloat16: AQ_BF16} if small else {k.dtype: _CODES[k.dtype]}
         self._ws = {}
         if not kv_workspace_bytes(self._c):
-            raise ValueError("unsupported cache: page_tokens must be a power of two in 8..1024 and "
-                             "head_dim a multiple of 16 up to 256")
+            raise ValueError("unsupported cache: page_tokens must be a power of two in 8..1024, "
+                             "head_dim a multiple of 16 up to 256, and no size may be 0")
 
     def _scratch(self, q_heads=0):
         # (stream, workspace address, bytes). One workspace per stream, as calls on different
