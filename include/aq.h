@@ -414,7 +414,8 @@ aq_status aq_store_destroy(aq_store* store);
  *     the lowest free indices. lens[s] is the length of sequence s (0: the slot s is unused);
  *     tables[s] holds its ceil(lens[s] / page_tokens) pages and -1 from there on.
  *   - A page held by several sequences is full: a fork shares full pages and copies a partial
- *     last page. Sequences only grow (until they are freed), so no shared page is ever written.
+ *     last page. Sequences only grow (until they are freed), so no new token's slot is in a
+ *     shared page.
  *   - 8-bit entries (dtype AQ_E4M3) have one scale per token and head, stored as the byte e + 127
  *     of the power of two 2^e that the code is multiplied by; e is the smallest exponent with
  *     max |x| <= 448 * 2^e, kept in [-60, 60], so that x / 2^e is exact and rounded once.
@@ -492,7 +493,8 @@ aq_status aq_kv_copy_pages(const aq_kv_cache* cache, int n, const int32_t* src, 
  *                16-byte aligned
  *   row_stride : elements from one row to the next, >= kv_heads * head_dim and a multiple of 8
  *                (the keys and values may be parts of one wider matrix)
- * No slot may be named twice. A row whose slot is not in the cache (a position outside
+ * No slot may be named twice. A position in a page that other sequences hold as well (one from
+ * before a fork) changes for all of them. A row whose slot is not in the cache (a position outside
  * 0..lens-1, an index out of range) is skipped and AQ_ERR_INVALID_ARG recorded. */
 aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t* seqs,
                       const int32_t* positions, const void* k, const void* v, int x_dtype,
