@@ -347,59 +347,84 @@ __device__ __forceinline__ void write_partial(const Args& a, int tile, const Acc
 // The factor that brings a partial with maximum m to maximum top.
 __device__ __forceinline__ float rebase(float m, float top) { return m == -INFINITY ? 0.0f : exp2_fast(m - top); }
 
-// Row r of the `count` <= 32 partials of the list put together by a warp, in order, to output row
-// q_row, or to the partial dst (which may be one of the list: a row is read and written by one
-// warp). A lane takes four columns, BATCH partials are under way at a time. OWN: the CTA's own
-// pieces, in shared memory; otherwise partials of other CTAs, read through L2. Out of line: the
-// main loop keeps its registers to itself.
-template <bool OWN, int BATCH, int HD, int ROWS, int OS>
-__device__ __noinline__ void merge_row(const Args& a, const float* const* list, int count, int r, size_t q_row, float* dst) {
+// Rows r0, r0 + 8 (while below `rows`; NH of them) of the `count` <= 32 partials of the list put
+// together by a warp, in order, to output rows from q_row on, or to the partial dst (which may be one
+// of the list: a row is read and written by one warp). A lane takes four columns, BATCH partials are
+// under way at a time. OWN: the CTA's own pieces, in shared memory; otherwise partials of other
+// CTAs, read through L2. Out of line: the main loop keeps its registers to itself.
+template <bool OWN, int BATCH, int HD, int NH>
+__device__ __noinline__ void merge_rows(const Args& a, const float* const* list, int count, int r0, int rows, size_t q_row,
+                                        float* dst) {
+    constexpr int ROWS = 8 * NH, OS = HD + 4;
     const int lane = threadIdx.x & 31;
     auto load = [](const float* q) { return OWN ? *q : __ldcg(q); };
     auto load4 = [](const float* q) { return OWN ? *(const float4*)q : __ldcg((const float4*)q); };
-    const float* p = list[min(lane, count - 1)] + r;
-    float m = load(p), l = load(p + ROWS);
-    float4 v[BATCH];
-    auto fetch = [&](int at, int y0) {               // (past the end: the last one again)
+    const float* p = list[min(lane, count - 1)];
+    int r[NH];                                       // (past the end: the first row again, not stored)
+    float m[NH], l[NH];
 #pragma unroll
-        for (int y = 0; y < BATCH; ++y) v[y] = load4(list[min(y0 + y, count - 1)] + at);
+    for (int g = 0; g < NH; ++g) {
+        r[g] = r0 + 8 * g < rows ? r0 + 8 * g : r0;
+        m[g] = load(p + r[g]), l[g] = load(p + ROWS + r[g]);
+    }
+    float4 v[NH][BATCH];
+    const int col0 = 4 * (HD < 128 ? lane & (HD / 4 - 1) : lane);
+    auto fetch = [&](int c, int y0) {                // (past the end: the last one again)
+#pragma unroll
+        for (int y = 0; y < BATCH; ++y) {
+            const float* from = list[min(y0 + y, count - 1)] + 2 * ROWS + c + col0;
+#pragma unroll
+            for (int g = 0; g < NH; ++g) v[g][y] = load4(from + r[g] * OS);
+        }
     };
-    const int col0 = 4 * (HD < 128 ? lane & (HD / 4 - 1) : lane), at0 = 2 * ROWS + r * OS + col0;
-    fetch(at0, 0);                                   // before the maxima are known
-    if (lane >= count) m = -INFINITY, l = 0.0f;
-    float top = m;
+    fetch(0, 0);                                     // before the maxima are known
+    float f[NH], inv[NH];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-    const float f = rebase(m, top == -INFINITY ? 0.0f : top);
-    float sum = f * l;
+    for (int g = 0; g < NH; ++g) {
+        if (lane >= count) m[g] = -INFINITY, l[g] = 0.0f;
+        float top = m[g];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-    const float inv = inverse_sum(sum);
-    if (lane == 0) {
-        if (dst) dst[r] = top, dst[ROWS + r] = sum;
-        else if (a.lse) a.lse[q_row] = lse_of(top, sum);
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        f[g] = rebase(m[g], top == -INFINITY ? 0.0f : top);
+        float sum = f[g] * l[g];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        inv[g] = inverse_sum(sum);
+        if (lane == 0 && r0 + 8 * g < rows) {
+            if (dst) dst[r[g]] = top, dst[ROWS + r[g]] = sum;
+            else if (a.lse) a.lse[q_row + r[g]] = lse_of(top, sum);
+        }
     }
 #pragma unroll 1
     for (int c = 0; c < HD; c += 128) {
-        const int col = c + col0, at = at0 + c;
-        if (c > 0) fetch(at, 0);
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (c > 0) fetch(c, 0);
+        float4 o[NH];
+#pragma unroll
+        for (int g = 0; g < NH; ++g) o[g] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
         for (int y0 = 0;;) {
 #pragma unroll
-            for (int y = 0; y < BATCH; ++y) {
-                const float fy = __shfl_sync(~0u, f, (y0 + y) & 31);
-                if (y0 + y < count) o.x += fy * v[y].x, o.y += fy * v[y].y, o.z += fy * v[y].z, o.w += fy * v[y].w;
-            }
+            for (int y = 0; y < BATCH; ++y)
+#pragma unroll
+                for (int g = 0; g < NH; ++g) {
+                    const float fy = __shfl_sync(~0u, f[g], (y0 + y) & 31);
+                    const float4 w = v[g][y];
+                    if (y0 + y < count) o[g].x += fy * w.x, o[g].y += fy * w.y, o[g].z += fy * w.z, o[g].w += fy * w.w;
+                }
             y0 += BATCH;
             if (y0 >= count) break;
-            fetch(at, y0);
+            fetch(c, y0);
         }
-        if (dst) {
-            *(float4*)(dst + at) = o;
-        } else if (col < a.head_dim) {
-            store_out2(a, q_row, col, o.x * inv, o.y * inv);
-            store_out2(a, q_row, col + 2, o.z * inv, o.w * inv);
+#pragma unroll
+        for (int g = 0; g < NH; ++g) {
+            if (r0 + 8 * g >= rows) break;
+            const int col = c + col0;
+            if (dst) {
+                *(float4*)(dst + 2 * ROWS + r[g] * OS + col) = o[g];
+            } else if (col < a.head_dim) {
+                store_out2(a, q_row + r[g], col, o[g].x * inv[g], o[g].y * inv[g]);
+                store_out2(a, q_row + r[g], col + 2, o[g].z * inv[g], o[g].w * inv[g]);
+            }
         }
     }
 }
@@ -812,17 +837,18 @@ __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::W
             rest &= ~of_seg;
             const int seg_rows = __shfl_sync(~0u, rows, y0);
             int r = (warp - turn) & (kWarps - 1);
-            turn += seg_rows;
+            const int first_rows = min(seg_rows, 8);   // (the others come with them)
+            turn += first_rows;
             const size_t q_row = (size_t)__shfl_sync(~0u, entry, y0) * a.q_heads + __shfl_sync(~0u, head0, y0);
             const int w = __shfl_sync(~0u, which, y0);
             if (pass == 0 && threadIdx.x == y0) s.cross[w] = {j0, ctas, rows, q_row};
-            if (r >= seg_rows) continue;
+            if (r >= first_rows) continue;
             if (of_seg >> lane & 1)
                 list[__popc(of_seg & ((1u << lane) - 1))] = (const float*)(ring + (lane >> 1) * T::PER_WARP) + (lane & 1 ? 0 : T::RING / 4);
             __syncwarp();
             float* const dst = pass == 1 ? nullptr : a.part + ((size_t)blockIdx.x * 2 + w) * T::PART;
-            for (; r < seg_rows; r += kWarps)
-                merge_row<true, 4, HD, T::ROWS, T::OS>(a, list, __popc(of_seg), r, q_row + r, dst);
+            for (; r < first_rows; r += kWarps)
+                merge_rows<true, 4, HD, NH>(a, list, __popc(of_seg), r, seg_rows, q_row, dst);
             __syncwarp();
         }
         if (pass == 0 && crossing) {
@@ -858,9 +884,9 @@ __device__ __forceinline__ void finish(const Args& a, Shared<Tile<DT, HD, NH>::W
             if (lane < members) list[lane] = part(lane);
             __syncwarp();
             float* const dst = final ? nullptr : part(0);
-            for (int r = warp; r < x.rows; r += kWarps) {
-                if (members <= 4) merge_row<false, 4, HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, dst);
-                else merge_row<false, 20, HD, T::ROWS, T::OS>(a, list, members, r, x.q_row + r, dst);
+            for (int r = warp; r < min(x.rows, 8); r += kWarps) {
+                if (members <= 4) merge_rows<false, 4, HD, NH>(a, list, members, r, x.rows, x.q_row, dst);
+                else merge_rows<false, NH == 1 ? 20 : 16, HD, NH>(a, list, members, r, x.rows, x.q_row, dst);
             }
             __syncwarp();
             if (final) break;
