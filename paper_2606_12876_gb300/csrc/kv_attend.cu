@@ -23,8 +23,8 @@
 //     order of the tokens, so the result does not depend on scheduling.
 //
 // Measured on a GB300 (copy peak 6.79 TB/s): 48 sequences of 8192 to 32768 tokens, 8 heads of 128,
-// bf16 (3.5 GB): 506 us; one sequence of 131071 tokens, fp16: 85.9 us (6.25 TB/s); 64 sequences of
-// 17 to 2048 tokens: 28.8 us; 64 query heads over an E4M3 cache of 380 MB: 69.9 us (5.4 TB/s). What a
+// bf16 (3.5 GB): 507 us; one sequence of 131071 tokens, fp16: 86.0 us (6.24 TB/s); 64 sequences of
+// 17 to 2048 tokens: 28.6 us; 64 query heads over an E4M3 cache of 380 MB: 70.0 us (5.4 TB/s). What a
 // call costs beside its bytes, about 4 us until the first keys arrive (lengths, table, keys: three
 // dependent reads) and 5 to 8 us to merge and join, is latency.
 //
