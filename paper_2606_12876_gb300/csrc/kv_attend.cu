@@ -627,7 +627,7 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 }
             }
     }
-    // base-2 scores; masked ones are -inf
+    // base-2 scores, for E4M3 plus the value scale's exponent b; masked ones are -inf
     const bool edge = p.t < p.lo || p.t + T::CT > p.len;
     float vexp[TT][2], vfac[TT][2];                // b and 2^b of the tokens' value scales
     float top[NH][2];
@@ -655,7 +655,8 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 for (int x = 0; x < 2; ++x) {
                     float& v = s[tt][g][2 * h + x];
                     v = out ? -INFINITY : v * (DT == AQ_E4M3 ? factor[g][x] * kf : factor[g][x]);
-                    top[g][x] = fmaxf(top[g][x], DT == AQ_E4M3 ? v + vexp[tt][h] : v);
+                    if constexpr (DT == AQ_E4M3) v += vexp[tt][h];
+                    top[g][x] = fmaxf(top[g][x], v);
                 }
         }
     float sub[NH][2];
@@ -680,7 +681,8 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 for (int j = 0; j < HD / 16; ++j) acc.o[g][j][x] *= f, acc.o[g][j][2 + x] *= f;
             }
     }
-    // weights: p for the sum, p 2^b rounded to 16 bits for the product with V, as B fragments
+    // weights: p for the sum, p 2^b rounded to 16 bits for the product with V, as B fragments. E4M3: b is
+    // taken off after the maximum, so that p 2^b is at most 1 however s + b was rounded.
     uint32_t w[TT][NH][2];
 #pragma unroll
     for (int tt = 0; tt < TT; ++tt)
@@ -688,7 +690,9 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
         for (int g = 0; g < NH; ++g)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                float p0 = exp2_fast(s[tt][g][2 * h] - sub[g][0]), p1 = exp2_fast(s[tt][g][2 * h + 1] - sub[g][1]);
+                float p0 = s[tt][g][2 * h] - sub[g][0], p1 = s[tt][g][2 * h + 1] - sub[g][1];
+                if constexpr (DT == AQ_E4M3) p0 -= vexp[tt][h], p1 -= vexp[tt][h];
+                p0 = exp2_fast(p0), p1 = exp2_fast(p1);
                 acc.l[g][0] += p0;
                 acc.l[g][1] += p1;
                 if constexpr (DT == AQ_E4M3) p0 *= vfac[tt][h], p1 *= vfac[tt][h];
