@@ -522,8 +522,10 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  * scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
  * the longest possible length, and AQ_ERR_INVALID_ARG recorded.
  * Accuracy: scores, maxima, sums and accumulators are fp32; the softmax weights are rounded to
- * the cache's 16-bit type (fp16 for AQ_E4M3) for the product with V: an error of at most 2^-8
- * (bf16) or 2^-11 (fp16) of sum_t p_t |v_t| / sum_t p_t before out is rounded. */
+ * the cache's 16-bit type (fp16 for AQ_E4M3) for the product with V. Before out is rounded that is
+ * an error of at most 2^-8 (bf16) or 2^-11 (fp16) of sum_t p_t |v_t| / sum_t p_t, and for fp16
+ * weights 2^-40 max_t (p_t b_t) sum_t |v_t| / b_t / sum_t p_t beside (b_t: the value's scale in
+ * AQ_E4M3, else 1). */
 size_t aq_kv_attend_workspace_bytes(const aq_kv_cache* cache, int n, int q_heads);
 aq_status aq_kv_attend(const aq_kv_cache* cache, int layer, int n, const int32_t* seqs, const void* q,
                        int q_dtype, int64_t q_stride, int q_heads, float scale, int window, void* out,

@@ -34,7 +34,10 @@
 // the rounding of the 16-bit output); their sum is taken before that rounding. E4M3 entries widen
 // exactly to fp16; the query is scaled to fp16's range by a power of two. A key's scale
 // multiplies its score; a value's scale 2^b multiplies its weight, with the running maximum taken
-// over s_t log2 e + b so that the fp16 weights stay in [0, 1].
+// over s_t log2 e + b so that p_t 2^b stays in [0, 1]. fp16 weights are taken times 2^15, fp16's range
+// above 1, so that those under a maximum keep their bits down to 2^-29 of it (with a maximum of 1
+// they were subnormal below 2^-14 and 0 below 2^-25, which many tokens under one large weight
+// notice); the output's division takes the factor back.
 #include <atomic>
 #include <climits>
 
@@ -48,6 +51,7 @@ constexpr int kMaxCtas = 160;
 constexpr size_t kArrivedBytes = 2048;                       // three counters per CTA
 static_assert(kArrivedBytes >= 3 * kMaxCtas * 4, "room for the counters");
 constexpr int kSliceSeqs = 512;       // sequences per launch (their offsets sit in shared memory)
+constexpr float kFp16Weights = 32768.0f;   // factor of fp16 weights (and so of their o)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Sizes for a cache type, a padded head dimension HD (64, 128 or 256) and NH groups of 8 heads.
@@ -87,6 +91,7 @@ struct Args {
     float* part;                      // [CTA][2][PART]: partials of segments that cross CTAs
     long long q_stride;
     float scale;
+    float o_scale;                    // 1 / the weights' factor
     int n, q_heads, kv_heads, group, tiles_per_head, head_dim, page_log2, num_pages, max_seqs, max_pages, window, q_dt;
 };
 
@@ -292,7 +297,7 @@ __device__ __forceinline__ void write_final(const Args& a, const Place& p, Acc<H
             const float l = column_sum(acc.l[g][x]);
             const int r = 8 * g + 2 * q + x;
             if (a.lse && lane < 4 && r < rows) a.lse[(size_t)p.i * a.q_heads + head0 + r] = lse_of(acc.m[g][x], l);
-            inv[x] = inverse_sum(l);
+            inv[x] = inverse_sum(l) * a.o_scale;
         }
         const int r = 8 * g + (lane >> 2);
         uint16_t* out = (uint16_t*)a.out + ((size_t)p.i * a.q_heads + head0 + r) * a.head_dim;
@@ -389,7 +394,7 @@ __device__ __noinline__ void merge_rows(const Args& a, const float* const* list,
         float sum = f[g] * l[g];
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-        inv[g] = inverse_sum(sum);
+        inv[g] = inverse_sum(sum) * a.o_scale;
         if (lane == 0 && r0 + 8 * g < rows) {
             if (dst) dst[r[g]] = top, dst[ROWS + r[g]] = sum;
             else if (a.lse) a.lse[q_row + r[g]] = lse_of(top, sum);
@@ -629,7 +634,7 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
     }
     // base-2 scores, for E4M3 plus the value scale's exponent b; masked ones are -inf
     const bool edge = p.t < p.lo || p.t + T::CT > p.len;
-    float vexp[TT][2], vfac[TT][2];                // b and 2^b of the tokens' value scales
+    float vexp[TT][2], vfac[TT][2];                // b and 2^b times the weights' factor of the tokens' value scales
     float top[NH][2];
 #pragma unroll
     for (int g = 0; g < NH; ++g) top[g][0] = top[g][1] = -INFINITY;
@@ -647,7 +652,7 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vb) : "r"(at + 64) : "memory");
                 kf = __uint_as_float(kb << 23);
                 vexp[tt][h] = (float)((int)vb - 127);
-                vfac[tt][h] = out ? 0.0f : __uint_as_float(vb << 23);   // (an unseen token's byte may be anything)
+                vfac[tt][h] = out ? 0.0f : __uint_as_float(vb << 23) * kFp16Weights;   // (an unseen token's byte may be anything)
             }
 #pragma unroll
             for (int g = 0; g < NH; ++g)
@@ -696,6 +701,7 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 acc.l[g][0] += p0;
                 acc.l[g][1] += p1;
                 if constexpr (DT == AQ_E4M3) p0 *= vfac[tt][h], p1 *= vfac[tt][h];
+                if constexpr (DT == AQ_F16) p0 *= kFp16Weights, p1 *= kFp16Weights;
                 w[tt][g][h] = transpose8x8(round_pack2<BF ? AQ_BF16 : AQ_F16>(p0, p1));
             }
     const uint32_t vt = stage + T::KV;
@@ -1074,6 +1080,7 @@ aq_status launch_kv_attend(const aq_kv_cache& c, const DeviceInfo& di, int layer
     a.out = out, a.lse = lse;
     a.status = (unsigned int*)ws;
     a.scale = scale;
+    a.o_scale = c.dtype == AQ_BF16 ? 1.0f : 1.0f / kFp16Weights;
     a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads / c.kv_heads;
     a.head_dim = c.head_dim;
     while ((1 << a.page_log2) < c.page_tokens) ++a.page_log2;

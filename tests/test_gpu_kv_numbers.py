@@ -1,9 +1,11 @@
-"""The numbers of aq_kv_attend where the weights or the scales are extreme, against fp64 within a bound
-that follows from its arithmetic: scores beyond 2^24, value and key scales at both ends of their range.
+"""The numbers of aq_kv_attend where the weights or the scales are extreme, against fp64 within the
+bound that aq.h states: long contexts under one token with most of the weight, scores beyond 2^24,
+value and key scales at both ends of their range.
 
-The bound: rounding the weights costs u sum_t p_t |v_t| / sum p, u = 2^-8 (bf16) or 2^-11 (fp16, E4M3), and
-for fp16 weights 2^-25 of the largest weight times scale for every token beside; a score's error d enters
-out twice (its own weight and the sum), and out is rounded once."""
+bound() is that statement and nothing else. With E the error of the weights' sum over v, p relative to
+their maximum, u = 2^-8 (bf16) or 2^-11 (fp16, E4M3) and b_t the value scales (1 without them):
+    E <= u sum_t p_t |v_t| / sum p  +  2^-40 max(p_t b_t) sum_t |v_t| / b_t / sum p     (no second term: bf16)
+a score's error d enters out twice (its own weight and the sum), and out is rounded once."""
 import pytest
 import torch
 
@@ -60,7 +62,7 @@ def bound(cache, q, scale):
     A = p @ v.abs()
     E = (2.0 ** -8 if cache.dtype == torch.bfloat16 else 2.0 ** -11) * A
     if cache.dtype != torch.bfloat16:
-        E = E + 2.0 ** -25 * (p * b[:, None]).amax(-1)[..., None] * (v.abs() / b[..., None]).sum(1)[:, None]
+        E = E + 2.0 ** -40 * (p * b[:, None]).amax(-1)[..., None] * (v.abs() / b[..., None]).sum(1)[:, None]
     e = (E + 2 * d[..., None] * A) * 1.01
     tol = e + K.UNIT[q.dtype] * (out.abs() + e) + K.TINY[q.dtype]
     return out, lse, tol, d + 2.0 ** -21 * lse.abs()
@@ -88,6 +90,46 @@ def unit_query(heads, dim, dtype):
     q = torch.zeros(1, heads, dim, device="cuda", dtype=dtype)
     q[..., 0] = 1
     return q
+
+
+# (1280 heads: a warp has a whole one, so that one maximum holds for all of its tokens)
+SIZES = [(2, 300, 64), (2, 131071, 64), (1280, 32760, 16)]
+
+
+@pytest.mark.parametrize("heads,n,dim", SIZES)
+@pytest.mark.parametrize("tail", ["flat", "normal"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "e4m3"])
+def test_a_long_tail_under_one_large_weight(dtype, tail, heads, n, dim):
+    """One token with a small value takes most of the weight; every other weight is about 2^-26 of it.
+    Together they make up a part of the sum that no output may lose."""
+    U.require_gpu()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    s = torch.zeros(heads, n, device="cuda")
+    if tail == "normal":
+        s.normal_(generator=g)
+    s[::2, 7] = s[1::2, n - 9] = 18
+    v = torch.randn(heads, n, dim, device="cuda", generator=g).mul_(0.25).add_(1)
+    v[::2, 7] = v[1::2, n - 9] = 2.0 ** -7
+    zero = torch.zeros(heads, n, device="cuda")
+    cache = cache_of(first_dim(s, dim), v, dtype, zero, zero)
+    group = 8 if heads == 2 else 1
+    for qd in [torch.float16, torch.bfloat16] if dtype == "e4m3" else [cache.dtype]:
+        check(cache, unit_query(group * heads, dim, qd))
+
+
+@pytest.mark.parametrize("heads,n,dim", SIZES)
+def test_a_large_value_scale_over_a_long_tail(heads, n, dim):
+    """E4M3: the largest weight times scale belongs to a token whose codes are 0; the others' are 2^-26 of it."""
+    U.require_gpu()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    v = torch.randn(heads, n, dim, device="cuda", generator=g).mul_(0.25).add_(1)
+    v[:, 3] = 0
+    v_exp = torch.zeros(heads, n, device="cuda")
+    v_exp[:, 3] = 26
+    cache = cache_of(first_dim(torch.zeros(heads, n, device="cuda"), dim), v, "e4m3", v_exp * 0, v_exp)
+    check(cache, unit_query(heads, dim, torch.float16))
 
 
 @pytest.mark.parametrize("n", [40, 5000])
