@@ -26,6 +26,16 @@ __device__ __forceinline__ uint16_t e4m3_pair(float first, float second) {
     return r;
 }
 
+// 16 bytes that are read once. A coherent load: the kernel ahead may have written them while this one
+// was already waiting for it (launch_dependent).
+__device__ __forceinline__ uint4 ld_once_v4(const void* p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                 : "l"(p));
+    return r;
+}
+
 // Eight consecutive elements of dtype dt (AQ_F16, AQ_BF16, AQ_F32) at element index i, widened to
 // fp32; 16-byte aligned. dt is the same for the whole grid, so the branches do not diverge.
 __device__ __forceinline__ void load8(const void* p, size_t i, int dt, float (&f)[8]) {

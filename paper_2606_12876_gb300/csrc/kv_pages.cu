@@ -297,7 +297,7 @@ __device__ void copy_pages(const aq_kv_cache& c, int count, const int* src, cons
         uint4 v[kCopyVecs];
 #pragma unroll
         for (int j = 0; j < kCopyVecs; ++j)
-            if (at + (size_t)j * kCopyThreads * 16 < page_bytes) v[j] = ld_stream_v4(p + at + (size_t)j * kCopyThreads * 16);
+            if (at + (size_t)j * kCopyThreads * 16 < page_bytes) v[j] = ld_once_v4(p + at + (size_t)j * kCopyThreads * 16);
 #pragma unroll
         for (int j = 0; j < kCopyVecs; ++j)
             if (at + (size_t)j * kCopyThreads * 16 < page_bytes) *(uint4*)(q + at + (size_t)j * kCopyThreads * 16) = v[j];
