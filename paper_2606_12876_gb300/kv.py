@@ -212,10 +212,13 @@ class PagedKVCache:
         return s[0] if n > 1 else heads * dim
 
     def check(self):
-        """Synchronise the streams that used the cache and raise AQError if a call recorded a
-        condition (AQ_ERR_CAPACITY: no free page or a full table; AQ_ERR_INVALID_ARG)."""
+        """Synchronise the device (a captured call may have been replayed on any stream) and raise
+        AQError if a call recorded a condition (AQ_ERR_CAPACITY: no free page or a full table;
+        AQ_ERR_INVALID_ARG)."""
         bad = AQ_OK
-        for stream, _, _, ws in self._ws.values():
-            bad = aq_workspace_status(ws, stream) or bad
+        with torch.cuda.device(self.device):
+            torch.cuda.synchronize()
+            for _, _, _, ws in self._ws.values():
+                bad = aq_workspace_status(ws) or bad
         if bad != AQ_OK:
             raise AQError(bad, "PagedKVCache")
