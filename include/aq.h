@@ -13,8 +13,8 @@
  *
  * Conventions that hold for every entry point:
  *   - All data pointers are DEVICE pointers, 16-byte aligned, owned by the caller. Apart
- *     from the aq_store_* entry points (dynamic loading, below), the library allocates and
- *     frees nothing and keeps no pointer after a call returns.
+ *     from the aq_store_* entry points (dynamic loading, below) and aq_workspace_create, the
+ *     library allocates and frees nothing and keeps no pointer after a call returns.
  *   - stream is a cudaStream_t passed as void* (NULL = the legacy default stream). All work
  *     is enqueued asynchronously on it; no call synchronises unless its comment says so.
  *   - Argument errors are detected on the host before anything is launched; the call then
@@ -580,6 +580,20 @@ aq_status aq_selftest_wait(void* workspace, size_t workspace_bytes, void* stream
 aq_status aq_selftest_read(const void* src, size_t bytes, void* sink, void* stream);
 aq_status aq_workspace_init(void* workspace, size_t bytes, void* stream);
 aq_status aq_workspace_status(void* workspace, void* stream);
+
+/* Workspaces for captured calls. A graph keeps the workspaces that its calls were captured with, and
+ * may be replayed on any stream: a workspace that a call must have to itself then belongs to one
+ * stream of one capture, not to the stream that the capture was made on.
+ * aq_workspace_create: *workspace receives bytes (> 0) of zero-filled device memory on the current
+ * device, 16-byte aligned. It may be called while the thread is capturing: neither the allocation nor
+ * the zero-fill becomes part of the graph; both have finished on return.
+ * aq_workspace_destroy: releases it (NULL: does nothing). No work may still use it.
+ * aq_capture_id: *id receives a number that no other capture of the process has if stream is being
+ * captured, else 0.
+ * Errors: AQ_ERR_INVALID_ARG, AQ_ERR_CUDA. */
+aq_status aq_workspace_create(size_t bytes, void** workspace);
+aq_status aq_workspace_destroy(void* workspace);
+aq_status aq_capture_id(void* stream, unsigned long long* id);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@ functions raise if the library is missing.
 """
 import ctypes
 import os
+import weakref
 
 import torch
 
@@ -32,7 +33,8 @@ EXPORTS = ["aq_abi_version", "aq_status_string", "aq_last_error", "aq_plane_byte
            "aq_gemv_group",
            "aq_kv_workspace_bytes", "aq_kv_init", "aq_kv_reserve", "aq_kv_fork", "aq_kv_free",
            "aq_kv_compact", "aq_kv_copy_pages", "aq_kv_write", "aq_kv_attend_workspace_bytes",
-           "aq_kv_attend", "aq_rmsnorm"]
+           "aq_kv_attend", "aq_rmsnorm", "aq_workspace_create", "aq_workspace_destroy",
+           "aq_capture_id"]
 
 
 class AQError(RuntimeError):
@@ -131,6 +133,11 @@ def lib():
             "aq_rmsnorm": (i32, [i32, i32, vp, i32, i64, vp, vp, i32, vp, i32, f32, vp, i32, vp,
                                  i32, vp]),
         })
+        sig.update({
+            "aq_workspace_create": (i32, [sz, ctypes.POINTER(vp)]),
+            "aq_workspace_destroy": (i32, [vp]),
+            "aq_capture_id": (i32, [vp, ctypes.POINTER(ctypes.c_ulonglong)]),
+        })
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = res, args
@@ -156,6 +163,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
 
 
 def _stream_of(index):
@@ -399,3 +407,31 @@ def aq_workspace_status(workspace, stream=None):
 def workspace(nbytes, device="cuda"):
     """A zero-filled workspace tensor of at least nbytes (16-byte aligned by the allocator)."""
     return torch.zeros(max(16, (nbytes + 15) // 16 * 16), dtype=torch.uint8, device=device)
+
+
+def capture_id(stream=None):
+    """A number of the capture that the stream is part of, or 0."""
+    n = ctypes.c_ulonglong()
+    _check(lib().aq_capture_id(_stream(stream), ctypes.byref(n)), "aq_capture_id")
+    return n.value
+
+
+class CaptureWorkspace:
+    """A zero-filled workspace of at least nbytes for the calls of one capture, made while it is under
+    way (aq_workspace_create); released with this object. Stands in for a workspace tensor."""
+
+    def __init__(self, nbytes):
+        p, n = ctypes.c_void_p(), max(16, (nbytes + 15) // 16 * 16)
+        _check(lib().aq_workspace_create(n, ctypes.byref(p)), "aq_workspace_create")
+        self._at, self._bytes = p.value, n
+        # (at exit the driver releases it)
+        weakref.finalize(self, lib().aq_workspace_destroy, p.value).atexit = False
+
+    def data_ptr(self):
+        return self._at
+
+    def numel(self):
+        return self._bytes
+
+    def element_size(self):
+        return 1

@@ -3,7 +3,10 @@
 Lists of sequences, counts, positions and pages are int32 tensors on the cache's device. Nothing
 synchronises: conditions found on the device (no free page, a bad index) are recorded and raised
 by check(). Work is enqueued on the current stream; calls that change the cache must not overlap
-other calls on it.
+other calls on it. Calls may be captured in CUDA graphs, on any stream, once the cache has been
+called outside a capture; a graph may be replayed on any stream, and graphs that only attend beside
+each other and beside eager calls. Every capture has workspaces of its own, a few MB that the cache
+keeps (so it has to outlive its graphs).
 """
 import ctypes
 
@@ -12,7 +15,7 @@ import torch
 from . import (AQ_BF16, AQ_E4M3, AQ_F16, AQ_F32, AQ_OK, AQError, KVCache, aq_kv_attend,
                aq_kv_compact, aq_kv_copy_pages, aq_kv_fork, aq_kv_free, aq_kv_init, aq_kv_reserve,
                aq_kv_write, aq_workspace_status, kv_attend_workspace_bytes, kv_workspace_bytes,
-               workspace, _stream_of)
+               workspace, CaptureWorkspace, capture_id, _capturing, _stream_of)
 
 _FLOATS = {torch.float16: AQ_F16, torch.bfloat16: AQ_BF16, torch.float32: AQ_F32}
 _CODES = dict(_FLOATS)
@@ -86,16 +89,19 @@ class PagedKVCache:
                              "head_dim a multiple of 16 up to 256, and no size may be 0")
 
     def _scratch(self, q_heads=0):
-        # (stream, workspace address, bytes). One workspace per stream, as calls on different
-        # streams may overlap; attention has its own (by query heads), page operations share one.
+        # (stream, workspace address, bytes, its owner). One workspace per stream for eager calls, as
+        # calls on different streams may overlap, and one per stream of a capture, as its graph may be
+        # replayed on any stream; attention has its own (by query heads), page operations share one.
         stream = _stream_of(self._index)
-        got = self._ws.get((stream, q_heads))
+        capturing = _capturing()
+        key = (stream, q_heads, capture_id(stream)) if capturing else (stream, q_heads)
+        got = self._ws.get(key)
         if got is None:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the first call on a stream allocates a workspace: make one before capturing")
+            if capturing and not self._ws:
+                raise RuntimeError("the cache's first call is inside a capture: make one outside before, on any stream")
             n = kv_attend_workspace_bytes(self._c, 1, q_heads) if q_heads else kv_workspace_bytes(self._c)
-            ws = workspace(n, self.device)
-            got = self._ws[(stream, q_heads)] = (stream, ws.data_ptr(), ws.numel(), ws)
+            ws = CaptureWorkspace(n) if capturing else workspace(n, self.device)
+            got = self._ws[key] = (stream, ws.data_ptr(), ws.numel(), ws)
         return got
 
     def _pages(self, call, *args):
