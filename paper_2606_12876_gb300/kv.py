@@ -93,7 +93,7 @@ class PagedKVCache:
         # calls on different streams may overlap, and one per stream of a capture, as its graph may be
         # replayed on any stream; attention has its own (by query heads), page operations share one.
         stream = _stream_of(self._index)
-        capturing = _capturing()
+        capturing = stream != 0 and _capturing()
         key = (stream, q_heads, capture_id(stream)) if capturing else (stream, q_heads)
         got = self._ws.get(key)
         if got is None:

@@ -1,4 +1,6 @@
 """Captured calls of a PagedKVCache: what a graph records and where it may be replayed."""
+import gc
+
 import pytest
 import torch
 
@@ -8,6 +10,15 @@ from paper_2606_12876_gb300 import AQ_ERR_INVALID_ARG, AQError
 from paper_2606_12876_gb300.kv import PagedKVCache
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def collected():
+    """Destroying a graph invalidates a capture that is under way: none of an earlier test's is left for the
+    collector to find then."""
+    gc.collect()
+    yield
+    gc.collect()
 
 
 def query(n, heads, dim, dtype, seed=0):
@@ -190,6 +201,34 @@ def test_graphs_replayed_at_once():
         for o, w in zip(outs, want):
             assert all(torch.equal(t, w) for t in o)
     cache.check()
+
+
+def test_a_cache_may_go_while_another_captures():
+    """The garbage collector may drop a cache with captured calls at any time, in the middle of a capture
+    too: releasing its workspaces must not disturb that."""
+    U.require_gpu()
+    q = query(1, 4, 64, torch.float16)
+
+    def used():
+        cache = PagedKVCache(4, 16, 1, 64, 1, dtype="f16")
+        cache.attend(q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.attend(q)
+        return cache, graph
+
+    old, old_graph = used()
+    old_graph.replay()
+    torch.cuda.synchronize()
+    del old_graph
+    cache, x, graph = used()[0], torch.zeros(4, device="cuda"), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        del old
+        out = cache.attend(q)
+    graph.replay()
+    assert x.tolist() == [1] * 4 and not bool(out.any())
 
 
 def test_workspaces_go_with_their_cache():
