@@ -17,11 +17,29 @@ from . import (AQ_BF16, AQ_F16, AQ_F32, AQ_LAYOUT_STATIC_WEIGHTS, DTYPES, TORCH_
                wmse_workspace_bytes, aq_workspace_init,
                aq_store_device_bytes, aq_store_planes, aq_store_scales, aq_store_set_prefix,
                gemm_workspace_bytes, gemv_workspace_bytes, lib, packed_bytes,
-               workspace, _stream)
+               workspace, CaptureWorkspace, capture_id, _capturing, _stream)
 
 
 def _destroy_store(store):
     lib().aq_store_destroy(store)
+
+
+# Workspaces of captured calls, by capture, stream in it, kind of call, layouts and size. A graph keeps
+# the addresses it was captured with and may be replayed on any stream, so none of them is shared
+# with another capture or with eager calls. Layers of the same layout share one within a capture (a model's
+# blocks), and hold it: it is released with the last of them.
+_capture_ws = weakref.WeakValueDictionary()
+
+
+def _capture_workspace(layers, kind, stream, nbytes):
+    layouts = tuple(tuple(getattr(lin.layout, f) for f, _ in Layout._fields_) for lin in layers)
+    key = (capture_id(stream), stream, kind, layouts, nbytes)
+    ws = _capture_ws.get(key)
+    if ws is None:
+        ws = _capture_ws[key] = CaptureWorkspace(nbytes)
+    for lin in layers:
+        lin._ws[key] = ws
+    return ws
 
 
 def _u16_to_device(a, device):
@@ -37,6 +55,10 @@ class AQLinear:
     scales: [out] bit patterns. The natural codes are packed on the GPU by aq_pack. After
     packing the stream is synchronised and the layout is marked AQ_LAYOUT_STATIC_WEIGHTS: the
     layer's weights are read-only from then on, so calls may prefetch them early.
+
+    Calls may be captured in CUDA graphs, which may be replayed on any stream and beside each other;
+    a capture's workspaces are its own and live as long as the layers (which have to outlive
+    their graphs).
     """
 
     def __init__(self, books, codes, scales, book_dtype="f16", scale_dtype="f16",
@@ -141,8 +163,12 @@ class AQLinear:
 
     def _workspace(self, kind, n):
         # One workspace per (kind, stream), grown on demand; GEMV calls (batch <= 16) also
-        # remember the size per batch, so a repeated call makes no size query.
+        # remember the size per batch, so a repeated call makes no size query. Captured calls:
+        # _capture_workspace.
         stream = _stream(None)
+        if stream != 0 and _capturing():
+            size = gemv_workspace_bytes if kind == "gemv" else gemm_workspace_bytes
+            return _capture_workspace([self], kind, stream, size(self.layout, n))
         key = (kind, stream)
         ws = self._ws.get(key)
         if kind == "gemv":
@@ -217,9 +243,13 @@ class AQLinear:
             raise TypeError("H must be float32 or bfloat16")
         d = torch.empty(self.M + (1 if lam is not None else 0), dtype=torch.float64,
                         device=self.device)
-        key = ("wmse", _stream(None))
-        ws = self._ws.get(key)
+        stream = _stream(None)
+        key = ("wmse", stream)
         nbytes = wmse_workspace_bytes(self.layout)
+        if stream != 0 and _capturing():
+            ws = _capture_workspace([self], "wmse", stream, nbytes)
+        else:
+            ws = self._ws.get(key)
         if ws is None or ws.numel() < nbytes:
             ws = workspace(nbytes, self.device)
             self._ws[key] = ws
@@ -245,8 +275,12 @@ def gemv_group(layers, x, m, ys=None, y_dtype=None):
     if ys is None:
         ys = [torch.empty(batch, lin.out, dtype=TORCH_DTYPES[yd], device=dev) for lin in layers]
     layouts = [lin.layout for lin in layers]
-    key = (tuple((lin.out, lin.inp, lin.M, lin.B) for lin in layers), batch, _stream(None), str(dev))
-    ws = _group_ws.get(key)
+    stream = _stream(None)
+    key = (tuple((lin.out, lin.inp, lin.M, lin.B) for lin in layers), batch, stream, str(dev))
+    if stream != 0 and _capturing():
+        ws = _capture_workspace(layers, "group", stream, gemv_group_workspace_bytes(layouts, batch))
+    else:
+        ws = _group_ws.get(key)
     if ws is None:
         ws = workspace(gemv_group_workspace_bytes(layouts, batch), dev)
         _group_ws[key] = ws
