@@ -41,7 +41,7 @@ def main():
     a = ap.parse_args()
     torch.manual_seed(0)
     blocks = build(a.blocks)
-    per_seq = -(-(a.context + a.steps + 8) // PAGE)   # (8: warm-up and capture)
+    per_seq = -(-(a.context + a.steps + 8) // PAGE)   # (8: warm-up)
     cache = PagedKVCache((a.beams + 1) * per_seq, PAGE, KV_HEADS, HEAD_DIM, a.beams + 1, per_seq, layers=a.blocks,
                          dtype=a.cache)
     ints = lambda v: torch.as_tensor(list(v), dtype=torch.int32, device="cuda")
@@ -69,12 +69,8 @@ def main():
     for _ in range(3):                               # warm-up; allocates the workspaces
         out = run()
     if a.graph:
-        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
-        side.wait_stream(torch.cuda.current_stream())
-        with torch.cuda.stream(side):
-            run()
-        torch.cuda.synchronize()
-        with torch.cuda.graph(graph, stream=side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
             out = run()
         run = graph.replay
     t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
