@@ -504,7 +504,9 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  *     s_t = scale * q . k_t,  out = sum_t p_t v_t / sum_t p_t,  p_t = exp(s_t - max s),
  *     lse = ln sum_t exp(s_t),       over t = max(0, L - window) .. L-1, L = lens[seqs[i]]
  * Query head h reads kv head h / (q_heads / kv_heads). A sequence of length 0 gives zeros and
- * lse = -inf (so does one whose scores are all -inf). Cached tokens that are not seen (past the length, before the window) are not read.
+ * lse = -inf (so does one whose scores are all -inf). Keys and values that are not seen (past the
+ * length, before the window) are not read; scale bytes beside those of tokens that are seen may be,
+ * and have no effect.
  *   q        : device, n rows of [q_heads][head_dim] of q_dtype, 16-byte aligned, q_stride
  *              elements apart (>= q_heads * head_dim, a multiple of 8); q_dtype is the cache's
  *              type, or AQ_F16 / AQ_BF16 for an AQ_E4M3 cache
@@ -517,7 +519,8 @@ aq_status aq_kv_write(const aq_kv_cache* cache, int layer, int n, const int32_t*
  *              zero-filled before first use and used by aq_kv_attend alone (it holds counters that
  *              every call leaves at zero); calls that may overlap must not share one.
  * seqs may name a sequence several times; NULL needs n <= max_seqs. One kernel per 512 entries:
- * the cache is read once, in equal shares of chunks of 16 to 64 tokens whatever the lengths are, and
+ * the cache is read once for every 16 query heads of a kv head (or fewer: 17 take two readings), in
+ * equal shares of chunks of 16 to 64 tokens whatever the lengths are, and
  * the shares' results are joined in the order of the tokens, so the result does not depend on
  * scheduling. A bad index or length in the cache's bookkeeping is read as no tokens, zeros or
  * the longest possible length, and AQ_ERR_INVALID_ARG recorded.

@@ -4,10 +4,12 @@
 //   o = sum_t p_t v_t / sum_t p_t with p_t = exp(s_t - max), lse = max + ln sum_t p_t,
 // in one pass over the cache with a running maximum and sum.
 //
-// Bound: every cached key and value is read once, 4 * head_dim bytes per token and head with
+// Bound: every cached key and value is read once per 16 query heads of its kv head, 4 * head_dim bytes per token and head with
 // 16-bit entries, for 4 * head_dim * (query heads per kv head) operations: a few operations per
 // byte, so HBM is the limit and the work is arranged around keeping loads in flight.
-//   - A tile is the up to 8 (or 16) query heads that share a kv head. mma.sync m16n8k16 takes 16
+//   - A tile is the up to 8 (or 16) query heads that share a kv head; above 16 there are several, each
+//     of which reads the kv head's tokens for itself (48 heads of 128 over one kv head, 131072 tokens:
+//     42.6 us, 16 heads 29.6). mma.sync m16n8k16 takes 16
 //     cached tokens as rows and 8 heads as columns, S^T = K Q^T, then 16 head dimensions as rows,
 //     O^T += V^T P^T: both big operands come straight from the copied tiles (ldmatrix), the
 //     weights change from one form to the other by an 8x8 transpose in registers, and a column's
@@ -22,9 +24,9 @@
 //     per CTA; of the CTAs that a segment crosses, the last to finish joins their partials, in the
 //     order of the tokens, so the result does not depend on scheduling.
 //
-// Measured on a GB300 (copy peak 6.79 TB/s): 48 sequences of 8192 to 32768 tokens, 8 heads of 128,
-// bf16 (3.5 GB): 507 us; one sequence of 131071 tokens, fp16: 86.0 us (6.24 TB/s); 64 sequences of
-// 17 to 2048 tokens: 28.6 us; 64 query heads over an E4M3 cache of 380 MB: 70.0 us (5.4 TB/s). What a
+// Measured on a GB300 (copy peak 6.79 TB/s), medians in a CUDA graph: 48 sequences of 8192 to 32768
+// tokens, 8 heads of 128, bf16 (3.5 GB): 511 us; one sequence of 131071 tokens, fp16: 87 us (6.2 TB/s);
+// 64 sequences of 17 to 2048 tokens: 29.1 us; 64 query heads over an E4M3 cache of 380 MB: 70.4 us (5.4 TB/s). What a
 // call costs beside its bytes, about 4 us until the first keys arrive (lengths, table, keys: three
 // dependent reads) and 5 to 8 us to merge and join, is latency.
 //
@@ -64,7 +66,8 @@ struct Tile {
     static constexpr int KV = CT * RB;                       // bytes of a chunk's keys (or values)
     static constexpr int STAGE = 2 * KV + (ESZ == 1 ? 128 : 0);   // keys, values, scale bytes
     // Two stages a warp, 128 KB a CTA: with three the SMs' queues grow and some get their data
-    // later than others (a 3.5 GB cache 530 us, with two 511).
+    // later than others (a 3.5 GB cache 530 us, with two 511). Registers: none spill but 16-head tiles at a
+    // head dimension of 256 (255 registers, 92 bytes of stores in 16 bits, 134 in E4M3).
     static constexpr int NS = 2;
     static constexpr int ROWS = 8 * NH;                      // query heads of a tile
     static constexpr int OS = HD + 4;                        // floats from one row of a partial's o to the next

@@ -4,11 +4,11 @@
 // latency for one. A row stays in registers between the sum and the output, so nothing is read
 // twice (rows of more than 32768 columns are read again, through L2). Threads take vectors of eight
 // elements; all loads of a thread, the weight's too, are issued before the first use, and h is
-// written before the row's sum is known. Sums are fp32, over at most 32 elements in a thread and
-// then pairwise over lanes and warps.
+// written before the row's sum is known. Sums are fp32, over at most 32 elements in a thread (64 in
+// rows that are read again) and then pairwise over lanes and warps.
 //
-// Measured on a GB300, bf16 with a bf16 residual: 4096 x 8192 in 42.8 us (6.28 TB/s of 6.79), 100000 x
-// 128 in 15.4 us, 1 x 4096 in 2.1 us back to back.
+// Measured on a GB300, bf16 with a bf16 residual: 4096 x 8192 in 42.9 us (6.26 TB/s of 6.79), 100000 x
+// 128 in 15.4 us, 1 x 4096 in 2.2 us back to back.
 #include "kv.cuh"
 
 namespace aq {
@@ -238,8 +238,10 @@ aq_status launch_rmsnorm(int rows, int cols, const void* x, int x_dt, long long 
     // Threads per row. With few rows as many as there are vectors, as a row's latency is what
     // counts. With many rows each thread has four loads of each operand in flight (4096 x 8192
     // bf16 with residual: 42.8 us with four vectors a thread, 47.1 with two, 51.4 with one), two
-    // vectors where one of them is fp32 (2047 x 4096 with an fp32 residual, 8-bit output: 15.8 us,
-    // 23.1 with four, which spill). Rows of fewer than 32 vectors share a warp.
+    // vectors where one of them is fp32 (2047 x 4096 with an fp32 residual, 8-bit output: 15.9 us,
+    // 23.1 with four, which spill 80 to 164 bytes in the 64 registers that 1024 threads leave; the
+    // 16-bit form spills 20). Rows of 16385 to 32768 columns need four whatever the types are. Rows of
+    // fewer than 32 vectors share a warp.
     int vpt = 1;
     if (vecs <= 32) {
         a.row_threads = 1;

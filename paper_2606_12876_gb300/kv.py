@@ -151,7 +151,7 @@ class PagedKVCache:
 
     def write(self, k, v, seqs, positions=None, layer=0):
         """Store row i of k and v ([n][kv_heads][head_dim], fp16, bf16 or fp32; rows may be
-        strided) as token positions[i] of sequence seqs[i] (default: its last token)."""
+        strided, with the same stride in both) as token positions[i] of sequence seqs[i] (default: its last token)."""
         n = self._list(seqs, "seqs")
         at = None
         if positions is not None:
