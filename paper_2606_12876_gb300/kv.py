@@ -199,6 +199,8 @@ class PagedKVCache:
                     lse.get_device() != self._index or not lse.is_contiguous():
                 raise ValueError("lse must be a contiguous fp32 [n][q_heads] tensor")
             lse_at = lse.data_ptr()
+        if window > 0x7fffffff:                     # (longer than any sequence; the C call takes an int)
+            window = 0
         stream, ws, size, _ = self._scratch(q_heads)
         status = aq_kv_attend(self._ref, layer, n, seqs_at, q.data_ptr(), code, stride, q_heads,
                               self.head_dim ** -0.5 if scale is None else scale, window,

@@ -178,3 +178,11 @@ def test_scales_at_both_ends(kv_heads, n):
             q = torch.zeros(1, 4 * kv_heads, dim, device="cuda", dtype=torch.bfloat16)
             q[..., at] = gain
             check(cache, q)                      # (outputs of up to 2^69: bf16 holds them)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 40 + 1])
+def test_windows_longer_than_any_sequence(window):
+    U.require_gpu()
+    cache = K.filled_cache(PagedKVCache, [100, 7], 16, 2, 64, "bf16", seed=5)
+    q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+    assert torch.equal(cache.attend(q, window=window), cache.attend(q))
