@@ -4,13 +4,13 @@
 //   o = sum_t p_t v_t / sum_t p_t with p_t = exp(s_t - max), lse = max + ln sum_t p_t,
 // in one pass over the cache with a running maximum and sum.
 //
-// Bound: every cached key and value is read once per 16 query heads of its kv head, 4 * head_dim bytes per token and head with
-// 16-bit entries, for 4 * head_dim * (query heads per kv head) operations: a few operations per
-// byte, so HBM is the limit and the work is arranged around keeping loads in flight.
+// Bound: every cached key and value is read once per 16 query heads of its kv head, 4 * head_dim
+// bytes per token and head with 16-bit entries, for 4 * head_dim * (query heads per kv head)
+// operations: a few operations per byte, so HBM is the limit and the work is arranged around
+// keeping loads in flight.
 //   - A tile is the up to 8 (or 16) query heads that share a kv head; above 16 there are several, each
 //     of which reads the kv head's tokens for itself (48 heads of 128 over one kv head, 131072 tokens:
-//     42.6 us, 16 heads 29.6). mma.sync m16n8k16 takes 16
-//     cached tokens as rows and 8 heads as columns, S^T = K Q^T, then 16 head dimensions as rows,
+//     42.6 us, 16 heads 29.6). mma.sync m16n8k16 takes 16 cached tokens as rows and 8 heads as columns, S^T = K Q^T, then 16 head dimensions as rows,
 //     O^T += V^T P^T: both big operands come straight from the copied tiles (ldmatrix), the
 //     weights change from one form to the other by an 8x8 transpose in registers, and a column's
 //     statistics are per-lane values. (At the copy bandwidth an SM receives 24 bytes a cycle,
@@ -654,7 +654,8 @@ __device__ __forceinline__ void compute(const Place& p, uint32_t stage, int lane
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(kb) : "r"(at) : "memory");
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(vb) : "r"(at + 64) : "memory");
                 kf = __uint_as_float(kb << 23);
-                vexp[tt][h] = (float)((int)vb - 127);
+                // (a bad page's bytes are 0; taken as -127, a piece of them alone would have sums beyond fp32)
+                vexp[tt][h] = (float)max((int)vb - 127, -kScaleExpMax);
                 vfac[tt][h] = out ? 0.0f : __uint_as_float(vb << 23) * kFp16Weights;   // (an unseen token's byte may be anything)
             }
 #pragma unroll

@@ -186,3 +186,33 @@ def test_windows_longer_than_any_sequence(window):
     cache = K.filled_cache(PagedKVCache, [100, 7], 16, 2, 64, "bf16", seed=5)
     q = torch.randn(2, 4, 64, device="cuda").bfloat16()
     assert torch.equal(cache.attend(q, window=window), cache.attend(q))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n", [(1, 20000), (8, 700), (8, 40)])
+def test_tokens_on_bad_pages_are_zeros(dtype, heads, n):
+    """Table entries outside the pool in half of a sequence, all but its end or everywhere: recorded, and the same
+    as keys and values of zero, also where a warp's whole piece has no other tokens."""
+    U.require_gpu()
+    from paper_2606_12876_gb300 import AQ_ERR_INVALID_ARG, AQError
+    dim = 64
+    cache = K.filled_cache(PagedKVCache, [n], PAGE, heads, dim, dtype, seed=6)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    q = (torch.randn(1, 4 * heads, dim, device="cuda", generator=g) * 2).to(torch.float16 if dtype == "e4m3" else cache.dtype)
+    pages = -(-n // PAGE)
+    for bad in {max(pages - 1, 1), -(-pages // 2), pages}:
+        zeroed = K.filled_cache(PagedKVCache, [n], PAGE, heads, dim, dtype, seed=6)
+        at = zeroed.tables[0, :bad].long()
+        for t in (zeroed.k, zeroed.v):
+            t.view(torch.uint8)[:, at] = 0
+        want, want_lse, tol, tol_lse = K.attend_exact(zeroed, q, [0], 0, dim ** -0.5, 0)
+        cache.tables.copy_(zeroed.tables)
+        cache.tables[0, :bad] = 1 << 20
+        lse = torch.empty(1, 4 * heads, device="cuda")
+        out = cache.attend(q, lse=lse)
+        with pytest.raises(AQError) as e:
+            cache.check()
+        assert e.value.status == AQ_ERR_INVALID_ARG
+        assert bool(((out.double() - want).abs() <= tol).all()), bad
+        assert bool(((lse.double() - want_lse).abs() <= tol_lse).all()), bad
